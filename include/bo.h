@@ -24,9 +24,15 @@
  *               candidates, with a Pareto front per sample.
  *   bo_mll    — exact log marginal likelihood and its gradient, for fitting
  *               the hyperparameters on the host.
+ *   bo_token_logprobs, bo_route, bo_dispatch — what the search's objectives
+ *               are measured from: log probabilities of a served model's
+ *               answers, the router's choices and their grouping by model
+ *               ("Threshold router", load fractions and load distribution),
+ *               with the gradients that train the model and the router.
  *
  * Conventions shared by every entry point:
- *   - All floating-point arrays are fp32, row-major, contiguous.
+ *   - All floating-point arrays are fp32, row-major, contiguous, unless an
+ *     entry point says otherwise.
  *   - "device" pointers are HIP device memory on the current device; "host"
  *     pointers are ordinary host memory read before the call returns.
  *   - The caller owns every buffer it passes; the library never frees them.
@@ -506,6 +512,185 @@ bo_status bo_profile_read(double* posterior_ms, double* ehvi_ms, int64_t* calls,
 #define BO_PEAK_HBM_COPY 3
 #define BO_PEAK_MFMA_F16 4
 bo_status bo_measure_peak(int32_t what, int64_t iters, double* rate, void* stream);
+
+/*
+ * Served outputs: log probabilities, routing and dispatch.
+ *
+ * Paper: the threshold router (a query's score decides which model answers
+ * it), the load fractions that replace the thresholds in the search (S1), GPU
+ * availability (S3) and the load distribution over a model's replicas. The
+ * score and the quality of an answer are read off a model's log
+ * probabilities, the router sends each query (or each token of an expert
+ * model) to its best models, and the choices are grouped by model.
+ *
+ * These calls take logits of the type that the model gives them in. They keep
+ * no state, allocate nothing and may run on any number of streams at once;
+ * all are asynchronous and can be captured in a graph.
+ */
+#define BO_TYPE_F32 0
+#define BO_TYPE_BF16 1
+#define BO_TYPE_F16 2
+#define BO_MAX_ALTERNATIVES 64   /* alternatives of bo_token_logprobs      */
+#define BO_MAX_EXPERTS 1024      /* experts of bo_route, bo_route_grad, bo_dispatch */
+#define BO_MAX_CHOICES 32        /* experts chosen per row                 */
+
+/*
+ * bo_token_logprobs — per row of logits the log probability and rank of a
+ * given token, the entropy, and the most probable alternatives.
+ *
+ * With x_j = inv_temperature * l_j, m = max_j l_j,
+ *   s = sum_j exp(inv_temperature (l_j - m)),   lse = inv_temperature m + log s:
+ *   logprob = x_t - lse
+ *   rank    = 1 + #{l_j > l_t} + #{j < t : l_j = l_t}
+ *   entropy = log s - 1/s sum_j exp(x_j - inv_temperature m) (x_j - inv_temperature m)
+ *   stats   = (m, log s)
+ *   the `top` largest logits in falling order, the lowest index first among
+ *   equals: their indices and log probabilities.
+ * Sums are held in fp32, partial sums per lane; the order of summation is
+ * fixed, so a call repeats bit for bit.
+ *
+ * A logit of -inf is masked: probability 0, no rank, never an alternative.
+ * Alternatives that a row lacks are index -1, log probability -inf. A row
+ * with every logit masked gives logprob -inf, rank 0, entropy 0, stats
+ * (-inf, -inf). A masked token gives logprob -inf, rank 0. A token < 0 stands
+ * for none: logprob 0, rank 0. A token >= V gives logprob NaN, rank 0. A NaN
+ * or +inf logit makes the row's floating results NaN; NaN logits are never
+ * alternatives and never counted by a rank.
+ *
+ * logits   device [T][stride] of `type`, the first V of each row used;
+ *          aligned to its type, stride >= V (any when T <= 1)
+ * tokens   device int64 [T], or NULL: no row has a token
+ * inv_temperature  finite, > 0
+ * top      0..min(V, BO_MAX_ALTERNATIVES)
+ * logprob, entropy device [T] out;  rank device int32 [T] out
+ * stats    device [T][2] out (what the gradient takes)
+ * top_ids  device int32 [T][top] out; top_logprobs device [T][top] out
+ *          (both NULL when top = 0)
+ * workspace  device, aligned to 16 bytes, of at least
+ *          bo_token_logprobs_workspace(T, V, top) bytes (NULL when that is 0);
+ *          overwritten; calls that may overlap need one each
+ * T >= 0 (0 is a no-op), 1 <= V < 2^31.
+ * Asynchronous. Errors: INVALID_ARGUMENT, CAPACITY (top, V, T * splits past
+ * the grid), DEVICE.
+ */
+int64_t bo_token_logprobs_workspace(int64_t T, int64_t V, int32_t top);
+bo_status bo_token_logprobs(const void* logits, int32_t type, int64_t T, int64_t V,
+                            int64_t stride, const int64_t* tokens, float inv_temperature,
+                            int32_t top, float* logprob, int32_t* rank, float* entropy,
+                            float* stats, int32_t* top_ids, float* top_logprobs,
+                            void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * bo_token_logprobs_grad — the gradient of the logits from those of the log
+ * probability, the entropy and the alternatives' log probabilities.
+ *
+ * With u_j = x_j - lse, p_j = exp(u_j):
+ *   grad_l_j = inv_temperature ( g_t 1[j = t] + sum_i g_i 1[j = id_i]
+ *              - p_j (g_t + sum_i g_i + g_H (u_j + entropy)) )
+ * (g_t 0 for a row without a token, g_i 0 for an id of -1). A row with every
+ * logit masked has gradient 0; a token >= V, or NaN stats, give NaN.
+ *
+ * logits, type, T, V, stride, tokens, inv_temperature: as given to
+ *          bo_token_logprobs; stats, entropy: its outputs
+ * grad_logprob, grad_entropy device [T], or NULL: 0
+ * top_ids, grad_top device [T][top] (NULL when top = 0): ids in [0, V) or -1
+ *          (others are ignored)
+ * grad_logits device [T][grad_stride] of `type` out: the first V of each row
+ *          written, rounded once; may be logits itself (same stride), and may
+ *          not overlap it otherwise
+ * Asynchronous. Errors: INVALID_ARGUMENT, CAPACITY, DEVICE.
+ */
+bo_status bo_token_logprobs_grad(const void* logits, int32_t type, int64_t T, int64_t V,
+                                 int64_t stride, const int64_t* tokens, float inv_temperature,
+                                 const float* stats, const float* entropy,
+                                 const float* grad_logprob, const float* grad_entropy,
+                                 int32_t top, const int32_t* top_ids, const float* grad_top,
+                                 void* grad_logits, int64_t grad_stride, void* stream);
+
+/*
+ * bo_route — each row's best experts and their weights.
+ *
+ * Scores: s = softmax(l) over the row, or s = sigmoid(l). An expert is chosen
+ * by v = s + bias (by l where bias is NULL: the same order without its
+ * rounding); the bias balances the loads and does not enter the weights. With
+ * groups > 1 the experts fall into equal groups of consecutive ones, a group
+ * counts for the sum of its group_best largest s + bias, and only the
+ * top_groups best groups' experts can be chosen. Larger values come first,
+ * the lowest index among equals.
+ *   weight_i = scale s_i, or scale s_i / sum of the chosen s (renormalise).
+ * An expert with a logit of -inf (masked for the row), a bias of -inf
+ * (withdrawn), or a NaN in either is never chosen (as a member of a group it
+ * counts -inf); a NaN or +inf logit makes a softmax row NaN, and then none of
+ * its experts is chosen. Choices that a row lacks are id -1, weight 0. The
+ * weights of a renormalised row are formed relative to its largest chosen
+ * score, so they stay exact where the scores themselves underflow.
+ *
+ * logits device [T][stride] of `type`, the first E of each row used
+ * bias   device [E] or NULL
+ * top    1..min(BO_MAX_CHOICES, E / groups * top_groups)
+ * groups divides E; 1 <= top_groups <= groups; group_best 1 or 2, at most
+ *        E / groups
+ * scale  finite
+ * ids    device int32 [T][top] out, in falling order of v; weights device
+ *        [T][top] out
+ * 1 <= E <= BO_MAX_EXPERTS; T >= 0. Asynchronous.
+ * Errors: INVALID_ARGUMENT, CAPACITY, DEVICE.
+ */
+#define BO_SCORE_SOFTMAX 0
+#define BO_SCORE_SIGMOID 1
+bo_status bo_route(const void* logits, int32_t type, int64_t T, int32_t E, int64_t stride,
+                   const float* bias, int32_t score, int32_t top, int32_t groups,
+                   int32_t top_groups, int32_t group_best, int32_t renormalise, float scale,
+                   int32_t* ids, float* weights, void* stream);
+
+/*
+ * bo_route_grad — the gradient of the router's logits from the weights'.
+ *
+ * The choice itself has no gradient; with w the weights, g their gradients
+ * and i over the chosen:
+ *   softmax, renormalised: grad_i = w_i (g_i - sum_k w_k g_k / scale)
+ *   sigmoid, renormalised: the same times (1 - s_i)
+ *   softmax: grad_j = scale s_j (g_j 1[j chosen] - sum_k s_k g_k)
+ *   sigmoid: grad_i = scale g_i s_i (1 - s_i)
+ * and 0 for the others, and for a row with no choice.
+ *
+ * ids          device int32 [T][top]: distinct within a row; ids outside
+ *              [0, E) stand for no choice
+ * grad_weights device [T][top]
+ * grad_logits  device [T][grad_stride] of `type` out: the first E of each row
+ *              written, rounded once; may be logits itself (same stride), and
+ *              may not overlap it otherwise
+ * Other arguments as bo_route. Asynchronous.
+ * Errors: INVALID_ARGUMENT, CAPACITY, DEVICE.
+ */
+bo_status bo_route_grad(const void* logits, int32_t type, int64_t T, int32_t E, int64_t stride,
+                        int32_t score, int32_t top, int32_t renormalise, float scale,
+                        const int32_t* ids, const float* grad_weights, void* grad_logits,
+                        int64_t grad_stride, void* stream);
+
+/*
+ * bo_dispatch — the choices grouped by expert.
+ *
+ * Pair p (row p / top, choice p % top of the ids) goes to expert ids[p]; an id
+ * outside [0, E) goes nowhere. Each expert takes its pairs in rising order of
+ * p, at most `capacity` of them when that is > 0.
+ *   load[e]    = pairs that asked for e (before the capacity)
+ *   offsets[e] = pairs kept by experts below e; offsets[E] = pairs kept
+ *   order      = the kept pairs, by expert, then p; -1 from offsets[E] on
+ *   position[p] = where p stands in order, or -1
+ *
+ * ids device int32 [N] (N = T * top, 0 <= N < 2^31 - 65536)
+ * load device int32 [E], offsets device int32 [E + 1], order, position
+ *        device int32 [N], all out
+ * workspace  device, aligned to 16 bytes, of at least
+ *        bo_dispatch_workspace(N, E) bytes (NULL when that is 0); overwritten;
+ *        calls that may overlap need one each
+ * Asynchronous. Errors: INVALID_ARGUMENT, CAPACITY, DEVICE.
+ */
+int64_t bo_dispatch_workspace(int64_t N, int32_t E);
+bo_status bo_dispatch(const int32_t* ids, int64_t N, int32_t E, int64_t capacity, int32_t* load,
+                      int32_t* offsets, int32_t* order, int32_t* position, void* workspace,
+                      int64_t workspace_bytes, void* stream);
 
 /* Releases a model (waits for its last stream first). NULL is a no-op. */
 void bo_free(bo_model model);

@@ -10,19 +10,22 @@ Functions mirror the C ABI in ``include/bo.h``:
 (``bo_mll``), ``score`` (``bo_score``, or ``bo_score_constrained`` when feasibility
 thresholds are given), ``nehvi_prepare`` / ``score_nehvi`` / ``Model.nehvi_front``
 (``bo_nehvi_prepare``, ``bo_score_nehvi``, ``bo_nehvi_front``), ``argmax``,
-``cholesky_test`` (device) and
+``cholesky_test`` (device), ``token_logprobs`` / ``token_logprobs_grad``, ``route``
+/ ``route_grad`` and ``dispatch`` (``bo_token_logprobs`` and so on) and
 ``pareto_front``, ``box_decomposition`` (host geometry, no GPU needed).
 """
 from __future__ import annotations
 
 import ctypes
 import os
-from typing import Optional
+from typing import NamedTuple, Optional
 
 import numpy as np
 
 __all__ = ["BoError", "Model", "lib", "lib_path", "fit", "fit_composite", "mll", "score", "score_noalloc", "nehvi_prepare", "score_nehvi", "argmax",
            "cholesky_test", "draw_fronts3_test", "profile_enable", "profile_read", "measure_peak", "pareto_front", "box_decomposition", "STATUS",
+           "TokenLogprobs", "token_logprobs", "token_logprobs_grad", "Routing", "route", "route_grad",
+           "Dispatch", "dispatch", "MAX_ALTERNATIVES", "MAX_EXPERTS", "MAX_CHOICES",
            "MAX_N", "MAX_D", "MAX_S", "MAX_BOXES"]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -35,6 +38,7 @@ STATUS = {
     6: "BO_ERR_NONFINITE_INPUT", 7: "BO_ERR_ILL_CONDITIONED",
 }
 MAX_N, MAX_D, MAX_S, MAX_BOXES = 2048, 32, 4096, 4096
+MAX_ALTERNATIVES, MAX_EXPERTS, MAX_CHOICES = 64, 1024, 32
 
 
 class BoError(RuntimeError):
@@ -102,6 +106,23 @@ def lib() -> ctypes.CDLL:
     L.bo_profile_read.restype = ctypes.c_int
     L.bo_measure_peak.argtypes = [i32, i64, ctypes.POINTER(ctypes.c_double), vp]
     L.bo_measure_peak.restype = ctypes.c_int
+    f32 = ctypes.c_float
+    L.bo_token_logprobs_workspace.argtypes = [i64, i64, i32]
+    L.bo_token_logprobs_workspace.restype = i64
+    L.bo_token_logprobs.argtypes = [vp, i32, i64, i64, i64, vp, f32, i32, vp, vp, vp, vp, vp, vp,
+                                    vp, i64, vp]
+    L.bo_token_logprobs.restype = ctypes.c_int
+    L.bo_token_logprobs_grad.argtypes = [vp, i32, i64, i64, i64, vp, f32, vp, vp, vp, vp, i32, vp,
+                                         vp, vp, i64, vp]
+    L.bo_token_logprobs_grad.restype = ctypes.c_int
+    L.bo_route.argtypes = [vp, i32, i64, i32, i64, vp, i32, i32, i32, i32, i32, i32, f32, vp, vp, vp]
+    L.bo_route.restype = ctypes.c_int
+    L.bo_route_grad.argtypes = [vp, i32, i64, i32, i64, i32, i32, i32, f32, vp, vp, vp, i64, vp]
+    L.bo_route_grad.restype = ctypes.c_int
+    L.bo_dispatch_workspace.argtypes = [i64, i32]
+    L.bo_dispatch_workspace.restype = i64
+    L.bo_dispatch.argtypes = [vp, i64, i32, i64, vp, vp, vp, vp, vp, i64, vp]
+    L.bo_dispatch.restype = ctypes.c_int
     L.bo_free.argtypes = [vp]
     L.bo_free.restype = None
     L.bo_status_string.argtypes = [ctypes.c_int]
@@ -398,6 +419,255 @@ def draw_fronts3_test(F, ref, lower=None, stream=None):
     fr, bx = front.cpu().numpy(), boxes.cpu().numpy()
     return ([fr[s, :c[S + s]].copy() for s in range(S)],
             [bx[s, :c[s]].copy() for s in range(S)])
+
+
+# ---- served outputs: log probabilities, routing, dispatch ----------------------
+
+class TokenLogprobs(NamedTuple):
+    """What token_logprobs returns, row by row: fp32 ``logprob``, ``entropy``
+    and ``stats`` [T, 2] (largest logit, log of the sum relative to it), int32
+    ``rank``, and the alternatives' int32 ``top_ids`` and fp32
+    ``top_logprobs`` [T, top]."""
+    logprob: object
+    rank: object
+    entropy: object
+    stats: object
+    top_ids: object
+    top_logprobs: object
+
+
+class Routing(NamedTuple):
+    """The chosen experts of each row, best first: int32 ``ids`` and fp32
+    ``weights`` [T, top] (id -1, weight 0 where a row has no more)."""
+    ids: object
+    weights: object
+
+
+class Dispatch(NamedTuple):
+    """Choices grouped by expert, all int32: ``load`` [E] asked for, ``offsets``
+    [E + 1] into ``order`` [N] (pair indices, -1 past offsets[E]), and
+    ``position`` (the shape of ids): each pair's place in order, or -1."""
+    load: object
+    offsets: object
+    order: object
+    position: object
+
+
+_TYPES = None
+
+
+def _types():
+    global _TYPES
+    if _TYPES is None:
+        import torch
+        _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+    return _TYPES
+
+
+def _rows(t, name):
+    """(pointer, type, T, columns, row stride) of a matrix whose rows are
+    contiguous and any distance apart."""
+    import torch
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor on the GPU")
+    if t.device.type != "cuda":
+        raise ValueError(f"{name} must live on a GPU (got {t.device})")
+    kind = _types().get(t.dtype)
+    if kind is None:
+        raise TypeError(f"{name} must be float32, bfloat16 or float16 (got {t.dtype})")
+    if t.dim() != 2:
+        raise ValueError(f"{name} must be a matrix (got {t.dim()} dimensions)")
+    T, C = t.shape
+    rs, cs = t.stride()
+    if cs != 1 and C > 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    if T > 1 and rs < C:
+        raise ValueError(f"{name} must have rows that do not overlap")
+    return t.data_ptr(), kind, T, C, rs if T > 1 else C
+
+
+def _vec(t, name, dtype, shape):
+    """Pointer of a contiguous GPU tensor of this type and shape."""
+    p = _dev(t, name, dtype)
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name} must have shape {shape} (got {tuple(t.shape)})")
+    return p
+
+
+class _On:
+    """Allocations made inside belong to the stream that the work runs on."""
+
+    def __init__(self, stream):
+        import torch
+        self.ctx = None if stream is None else torch.cuda.stream(stream)
+
+    def __enter__(self):
+        if self.ctx is not None:
+            self.ctx.__enter__()
+
+    def __exit__(self, *e):
+        if self.ctx is not None:
+            self.ctx.__exit__(*e)
+
+
+def _workspace(nbytes, device):
+    import torch
+    if nbytes == 0:
+        return None, None
+    w = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    return w, w.data_ptr()
+
+
+def token_logprobs(logits, tokens=None, top=0, inv_temperature=1.0, out=None, stream=None):
+    """bo_token_logprobs: logits [T, V] (fp32, bf16 or fp16 GPU tensor, rows
+    any distance apart), tokens int64 [T] (negative: none) or None. Returns a
+    TokenLogprobs; ``out`` takes one of the same shapes to write into."""
+    import torch
+    lp, kind, T, V, stride = _rows(logits, "logits")
+    top = int(top)
+    f32, i32, dev = torch.float32, torch.int32, logits.device
+    if top < 0:
+        raise ValueError("top must not be negative")
+    tp = None if tokens is None else _vec(tokens, "tokens", torch.int64, (T,))
+    L = lib()
+    with _On(stream):
+        if out is None:
+            out = TokenLogprobs(
+                torch.empty(T, dtype=f32, device=dev), torch.empty(T, dtype=i32, device=dev),
+                torch.empty(T, dtype=f32, device=dev), torch.empty((T, 2), dtype=f32, device=dev),
+                torch.empty((T, top), dtype=i32, device=dev),
+                torch.empty((T, top), dtype=f32, device=dev))
+            ptrs = [t.data_ptr() for t in out]
+        else:
+            ptrs = [_vec(t, n, d, s) for t, n, d, s in zip(
+                out, TokenLogprobs._fields, (f32, i32, f32, f32, i32, f32),
+                ((T,), (T,), (T,), (T, 2), (T, top), (T, top)))]
+        need = L.bo_token_logprobs_workspace(T, V, top)
+        ws, wp = _workspace(need, dev)
+        st = L.bo_token_logprobs(lp, kind, T, V, stride, tp, inv_temperature, top, *ptrs, wp, need,
+                                 _stream(stream))
+    _check(st, "bo_token_logprobs")
+    return out
+
+
+def token_logprobs_grad(logits, tokens, stats, entropy, grad_logprob=None, grad_entropy=None,
+                        top_ids=None, grad_top=None, inv_temperature=1.0, out=None, stream=None):
+    """bo_token_logprobs_grad: the gradient of the logits ([T, V], their type)
+    from those of token_logprobs' outputs; ``stats`` and ``entropy`` as it
+    returned them. ``out`` may be ``logits`` itself."""
+    import torch
+    lp, kind, T, V, stride = _rows(logits, "logits")
+    f32 = torch.float32
+    tp = None if tokens is None else _vec(tokens, "tokens", torch.int64, (T,))
+    sp, ep = _vec(stats, "stats", f32, (T, 2)), _vec(entropy, "entropy", f32, (T,))
+    gl = None if grad_logprob is None else _vec(grad_logprob, "grad_logprob", f32, (T,))
+    gh = None if grad_entropy is None else _vec(grad_entropy, "grad_entropy", f32, (T,))
+    if (top_ids is None) != (grad_top is None):
+        raise ValueError("top_ids and grad_top go together")
+    top, ip, gp = 0, None, None
+    if top_ids is not None:
+        top = top_ids.shape[-1]
+        ip, gp = _vec(top_ids, "top_ids", torch.int32, (T, top)), _vec(grad_top, "grad_top", f32, (T, top))
+    if out is None:
+        with _On(stream):
+            out = torch.empty((T, V), dtype=logits.dtype, device=logits.device)
+    op, okind, oT, oV, ostride = _rows(out, "out")
+    if (okind, oT, oV) != (kind, T, V):
+        raise ValueError("out must have the logits' shape and type")
+    st = lib().bo_token_logprobs_grad(lp, kind, T, V, stride, tp, inv_temperature, sp, ep, gl, gh,
+                                      top, ip, gp, op, ostride, _stream(stream))
+    _check(st, "bo_token_logprobs_grad")
+    return out
+
+
+_SCORES = {"softmax": 0, "sigmoid": 1}
+
+
+def _score(score):
+    if score not in _SCORES:
+        raise ValueError(f"score must be 'softmax' or 'sigmoid' (got {score!r})")
+    return _SCORES[score]
+
+
+def route(logits, top, bias=None, score="softmax", groups=1, top_groups=1, group_best=1,
+          renormalise=True, scale=1.0, out=None, stream=None):
+    """bo_route: each row of logits [T, E] (fp32, bf16 or fp16 GPU tensor, rows
+    any distance apart) is sent to its ``top`` best experts. ``bias`` fp32 [E]
+    enters the choice only (-inf withdraws an expert); with groups the choice
+    is limited to the ``top_groups`` best groups, by the sum of their
+    ``group_best`` largest values. Returns a Routing; ``out`` takes one of the
+    same shapes to write into."""
+    import torch
+    lp, kind, T, E, stride = _rows(logits, "logits")
+    top = int(top)
+    if top < 1:
+        raise ValueError("top must be at least 1")
+    sc = _score(score)
+    bp = None if bias is None else _vec(bias, "bias", torch.float32, (E,))
+    if out is None:
+        with _On(stream):
+            out = Routing(torch.empty((T, top), dtype=torch.int32, device=logits.device),
+                          torch.empty((T, top), dtype=torch.float32, device=logits.device))
+        ip, wp = out.ids.data_ptr(), out.weights.data_ptr()
+    else:
+        ip = _vec(out[0], "ids", torch.int32, (T, top))
+        wp = _vec(out[1], "weights", torch.float32, (T, top))
+    st = lib().bo_route(lp, kind, T, E, stride, bp, sc, top, groups, top_groups, group_best,
+                        1 if renormalise else 0, scale, ip, wp, _stream(stream))
+    _check(st, "bo_route")
+    return out
+
+
+def route_grad(logits, ids, grad_weights, score="softmax", renormalise=True, scale=1.0, out=None,
+               stream=None):
+    """bo_route_grad: the gradient of route's logits ([T, E], their type) from
+    that of its weights, for the ``ids`` it chose. ``out`` may be ``logits``
+    itself."""
+    import torch
+    lp, kind, T, E, stride = _rows(logits, "logits")
+    if not isinstance(ids, torch.Tensor) or ids.dim() != 2:
+        raise TypeError("ids must be an int32 matrix on the GPU")
+    top = ids.shape[1]
+    ip = _vec(ids, "ids", torch.int32, (T, top))
+    gp = _vec(grad_weights, "grad_weights", torch.float32, (T, top))
+    sc = _score(score)
+    if out is None:
+        with _On(stream):
+            out = torch.empty((T, E), dtype=logits.dtype, device=logits.device)
+    op, okind, oT, oE, ostride = _rows(out, "out")
+    if (okind, oT, oE) != (kind, T, E):
+        raise ValueError("out must have the logits' shape and type")
+    st = lib().bo_route_grad(lp, kind, T, E, stride, sc, top, 1 if renormalise else 0, scale, ip,
+                             gp, op, ostride, _stream(stream))
+    _check(st, "bo_route_grad")
+    return out
+
+
+def dispatch(ids, experts, capacity=0, out=None, stream=None):
+    """bo_dispatch: the choices ``ids`` (int32 GPU tensor of any shape, in
+    row-major order) grouped by expert, at most ``capacity`` each when that is
+    not 0. Returns a Dispatch; ``out`` takes one of the same shapes to write
+    into."""
+    import torch
+    idp = _dev(ids, "ids", torch.int32)
+    N, E, i32, dev = ids.numel(), int(experts), torch.int32, ids.device
+    if E < 1:
+        raise ValueError("experts must be at least 1")
+    L = lib()
+    with _On(stream):
+        if out is None:
+            out = Dispatch(torch.empty(E, dtype=i32, device=dev),
+                           torch.empty(E + 1, dtype=i32, device=dev),
+                           torch.empty(N, dtype=i32, device=dev), torch.empty_like(ids))
+            ptrs = [t.data_ptr() for t in out]
+        else:
+            ptrs = [_vec(t, n, i32, s) for t, n, s in zip(
+                out, Dispatch._fields, ((E,), (E + 1,), (N,), tuple(ids.shape)))]
+        need = L.bo_dispatch_workspace(N, E)
+        ws, wp = _workspace(need, dev)
+        st = L.bo_dispatch(idp, N, E, capacity, *ptrs, wp, need, _stream(stream))
+    _check(st, "bo_dispatch")
+    return out
 
 
 def pareto_front(Y, ref: Optional[np.ndarray] = None) -> np.ndarray:

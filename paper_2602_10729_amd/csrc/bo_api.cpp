@@ -38,6 +38,7 @@ bool sync_debug() {
 }
 
 constexpr size_t kLdsLimit = 160 * 1024;
+}  // namespace
 
 // Device pointer check: the whole [p, p + bytes) must lie in one device
 // allocation of the current device.
@@ -84,7 +85,7 @@ bo_status after_launch(hipError_t e, hipStream_t st, const char* what) {
   return BO_OK;
 }
 
-
+namespace {
 bool all_finite(const float* v, size_t n) {
   for (size_t i = 0; i < n; ++i)
     if (!std::isfinite(v[i])) return false;

@@ -27,6 +27,10 @@ bo_status noalloc_scratch(int dev, float** out);
 // Thread-local error detail; returns the status for chaining.
 bo_status fail(bo_status st, const std::string& msg);
 bo_status hip_fail(hipError_t e, const char* what);
+// The whole [p, p + bytes) must lie in one device allocation of the current
+// device; the status of a launch (with BO_SYNC_DEBUG=1 of the work too).
+bo_status check_dev(const void* p, size_t bytes, const char* name);
+bo_status after_launch(hipError_t e, hipStream_t st, const char* what);
 
 // Host geometry (host_geom.cpp) -------------------------------------------
 // Non-dominated rows of Y (maximise, duplicates keep the lowest index),
