@@ -1,8 +1,19 @@
 // Log probabilities of given tokens, entropy, ranks and alternatives, and the
 // gradient of the logits.
 //
-// One workgroup per row: the maximum, then the sums relative to it, then one
-// sweep per alternative for the largest (value, lowest index) below the last.
+// Forward, one pass over a row: a lane keeps a reference r near its largest
+// logit, s = sum exp2(t) and w = sum t exp2(t) with t = c (l - r), c =
+// log2(e) / temperature; lanes are joined by moving their sums to the row's
+// maximum M:
+//   s' = s 2^d,  w' = (w + d s) 2^d,  d = c (r - M).
+// The largest logits are collected on the way: a workgroup knows a threshold
+// that at least `top` logits of the row reach, appends what lies above it to a
+// list in LDS, and now and then keeps the list's `top` best, whose last raises
+// the threshold. A row's first chunk sets it from its lanes' maxima. What is
+// appended falls off with the place in the row, about top / chunk number a
+// chunk, so the search costs one comparison of a vector's maximum.
+#include <algorithm>
+
 #include "serving.h"
 
 namespace bo {
@@ -14,87 +25,343 @@ constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
 // A finite stand-in for -inf where it is multiplied by a probability of 0.
 constexpr float kLow = -1e30f;
+constexpr int kChunk = 32;               // elements a thread holds at once
+constexpr int kCand = 768;               // room for appended candidates
+constexpr int kMergeAt = 32;             // candidates that are worth a merge
+// A lane's reference follows its maximum when that is this far above (in
+// powers of two): exp2 stays below 2^4 and few chunks pay for a rescale.
+constexpr float kSlack = 4.0f;
 
-// Orders (value, index): larger value first, lower index among equals; the
-// unsigned order of the result is the wanted one. -0 and +0 are equal.
-__device__ __forceinline__ unsigned long long pack_key(float v, unsigned j) {
+// max of three; NaN operands are dropped (a signalling one may come through)
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
+  return d;
+}
+__device__ __forceinline__ float max2(float a, float b) {
+  float d;
+  asm("v_max_f32 %0, %1, %2" : "=v"(d) : "v"(a), "v"(b));
+  return d;
+}
+
+// The largest fp32 value below v (v finite or +inf).
+__device__ __forceinline__ float below(float v) {
   const unsigned u = __float_as_uint(v + 0.0f);
-  const unsigned o = (u & 0x80000000u) ? ~u : (u | 0x80000000u);
-  return (static_cast<unsigned long long>(o) << 32) | (0xFFFFFFFFu - j);
-}
-__device__ __forceinline__ float key_value(unsigned long long k) {
-  const unsigned o = static_cast<unsigned>(k >> 32);
-  return __uint_as_float((o & 0x80000000u) ? (o & 0x7FFFFFFFu) : ~o);
+  if (v == 0.0f) return __uint_as_float(0x80000001u);
+  return __uint_as_float(v > 0.0f ? u - 1 : u + 1);
 }
 
-template <typename V, typename F>
-__device__ V block_reduce(V v, V* lds, F f) {
-  for (int off = 32; off > 0; off >>= 1) v = f(v, __shfl_xor(v, off));
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = lds[0];
-  for (int i = 1; i < kWg / 64; ++i) v = f(v, lds[i]);
+__device__ __forceinline__ float wave_max(float v) {
+  for (int off = 32; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor(v, off));
+  return v;
+}
+__device__ __forceinline__ float wave_sum(float v) {
+  for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off);
   return v;
 }
 
-template <int TYPE>
-__global__ __launch_bounds__(kWg) void k_logprobs(LogprobArgs a) {
+// (s, w) relative to r, moved to M >= r: a lane without a finite logit has
+// r = -inf and s = 0 (or NaN, which stays).
+__device__ __forceinline__ void move_to(float M, float r, float c, float& s, float& w) {
+  if (r == kNegInf) return;
+  const float d = fmaxf((r - M) * c, kLow), f = __builtin_amdgcn_exp2f(d);
+  w = (w + s * d) * f;
+  s *= f;
+  if (r != r || M - M != 0.0f) s = w = __builtin_nanf("");
+}
+
+struct Partial {      // of one row's share
+  float M, s, w;
+  int ahead;
+};
+
+// The row's outputs from its joined sums (one thread).
+__device__ __forceinline__ float finish(const LogprobArgs& a, int64_t row, const Partial& p,
+                                        int64_t tok, float xt) {
+  const bool has = tok >= 0 && tok < a.V;
+  const float ls = logf(p.s);
+  a.stats[2 * row] = p.M;
+  a.stats[2 * row + 1] = ls;
+  a.entropy[row] = p.M == kNegInf && p.s == 0.0f ? 0.0f : ls - p.w / p.s * kLn2;
+  float lp = 0.0f;
+  if (has) lp = xt == kNegInf && p.s == p.s ? kNegInf : (xt - p.M) * a.it - ls;
+  if (tok >= a.V) lp = __builtin_nanf("");
+  a.logprob[row] = lp;
+  a.rank[row] = has && xt > kNegInf ? p.ahead + 1 : 0;
+  return ls;
+}
+__device__ __forceinline__ void finish_top(const LogprobArgs& a, int64_t row, int i,
+                                           unsigned long long key, float M, float ls) {
+  a.top_ids[row * a.top + i] = key ? key_index(key) : -1;
+  a.top_logprobs[row * a.top + i] = key ? (key_value(key) - M) * a.it - ls : kNegInf;
+}
+
+struct TopLds {
+  unsigned long long list[2][BO_MAX_ALTERNATIVES];
+  unsigned long long cand[kCand];
+  unsigned lane_max[kWg];
+  float wave_th[kWg / 64];
+  int count[2];
+};
+
+// Keeps the k best of list[cur][0..kcur) and cand[0..n): each key's rank is
+// the number of larger ones. Ends with a barrier; returns how many are kept.
+__device__ int merge(TopLds& L, int cur, int kcur, int n, int k) {
+  __syncthreads();
+  const int all = kcur + n;
+  for (int i = threadIdx.x; i < all; i += kWg) {
+    const unsigned long long key = i < kcur ? L.list[cur][i] : L.cand[i - kcur];
+    int rank = 0;
+    for (int j = 0; j < kcur; ++j) rank += L.list[cur][j] > key;
+    for (int j = 0; j < n; ++j) rank += L.cand[j] > key;
+    if (rank < k) L.list[cur ^ 1][rank] = key;
+  }
+  __syncthreads();
+  return all < k ? all : k;
+}
+
+// One workgroup per (row, share of the row's chunks).
+template <int TYPE, bool TOP>
+__global__ __launch_bounds__(kWg) void k_logprobs(LogprobArgs a, int splits, int cps) {
   using El = Elem<TYPE>;
-  __shared__ float fl[kWg / 64];
+  using V = Vec<TYPE>;
+  constexpr int KV = V::kVec, U = kChunk / KV;
+  __shared__ float fl[3][kWg / 64];
   __shared__ int il[kWg / 64];
-  __shared__ unsigned long long ul[kWg / 64];
-  const auto add = [](auto x, auto y) { return x + y; };
-  const auto larger = [](auto x, auto y) { return x > y ? x : y; };
-  for (int64_t row = blockIdx.x; row < a.T; row += gridDim.x) {
+  __shared__ float row_ls;
+  __shared__ TopLds L;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int V_ = static_cast<int>(a.V), nv = (V_ - 1) / KV + 1;
+  const float c = a.it * kLog2e, slack = kSlack / c;
+  const int64_t work = a.T * splits;
+  for (int64_t g = blockIdx.x; g < work; g += gridDim.x) {
+    const int64_t row = splits == 1 ? g : g / splits;
+    const int part = splits == 1 ? 0 : static_cast<int>(g - row * splits);
     const typename El::T* x = static_cast<const typename El::T*>(a.logits) + row * a.stride;
     const int64_t tok = a.tokens ? a.tokens[row] : -1;
     const bool has = tok >= 0 && tok < a.V;
     const float xt = has ? El::load(x[tok]) : 0.0f;
-    float m = kNegInf;
-    for (int64_t j = threadIdx.x; j < a.V; j += kWg) m = fmaxf(m, El::load(x[j]));
-    m = block_reduce(m, fl, [](float p, float q) { return fmaxf(p, q); });
-    const float mr = m == kNegInf ? 0.0f : m, c = a.it * kLog2e;
-    float s = 0.0f, w = 0.0f;
-    int ahead = 0;
-    for (int64_t j = threadIdx.x; j < a.V; j += kWg) {
-      const float v = El::load(x[j]), t = (v - mr) * c, e = exp2f(t);
-      s += e;
-      w += e * fmaxf(t, kLow);
-      ahead += (v > xt || (v == xt && j < tok)) ? 1 : 0;
-    }
-    s = block_reduce(s, fl, add);
-    w = block_reduce(w, fl, add);
-    ahead = block_reduce(ahead, il, add);
-    const float ls = logf(s);
-    if (threadIdx.x == 0) {
-      a.stats[2 * row] = m;
-      a.stats[2 * row + 1] = ls;
-      a.entropy[row] = m == kNegInf && s == 0.0f ? 0.0f : ls - w / s * kLn2;
-      float lp = 0.0f;
-      if (has) lp = xt == kNegInf && s == s ? kNegInf : (xt - m) * a.it - ls;
-      if (tok >= a.V) lp = __builtin_nanf("");
-      a.logprob[row] = lp;
-      a.rank[row] = has && xt > kNegInf ? ahead + 1 : 0;
-    }
-    unsigned long long last = ~0ull;
-    for (int i = 0; i < a.top; ++i) {
-      unsigned long long best = 0ull;
-      for (int64_t j = threadIdx.x; j < a.V; j += kWg) {
-        const float v = El::load(x[j]);
-        if (v > kNegInf) {
-          const unsigned long long k = pack_key(v, static_cast<unsigned>(j));
-          if (k < last && k > best) best = k;
+    // what a logit must exceed to stand before the token: behind it and ahead
+    const float gt = has ? xt : __builtin_huge_valf(), ge = has ? below(xt) : gt;
+    const int tv = has ? static_cast<int>(tok) / KV : -1;  // the token's vector
+    const int v0 = min(nv, part * cps * (kWg * U)), v1 = min(nv, v0 + cps * (kWg * U));
+
+    float m = kNegInf, ref = kNegInf, rz = 0.0f, s = 0.0f, w = 0.0f;
+    int ahead = 0, ahead_lane = 0;
+    float th = kNegInf;
+    int cur = 0, kcur = 0, pending = 0, parity = 0;
+    int seen[2] = {0, 0};
+    if (TOP && tid < 2) L.count[tid] = 0;
+
+    for (int vb = v0; vb < v1; vb += kWg * U) {
+      V q[U];
+      float vm[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int v = vb + u * kWg + tid;
+        if (v < v1) {
+          const typename El::T* p = x + (int64_t)v * KV;
+          if (v < nv - 1 || V_ % KV == 0) q[u].load(p);
+          else q[u].load_part(p, V_ % KV);
+        } else {
+          q[u].fill_masked();
         }
       }
-      best = block_reduce(best, ul, larger);
-      if (threadIdx.x == 0) {
-        const float v = key_value(best);
-        a.top_ids[row * a.top + i] = best ? static_cast<int>(0xFFFFFFFFu - static_cast<unsigned>(best)) : -1;
-        a.top_logprobs[row * a.top + i] = best ? (v - m) * a.it - ls : kNegInf;
+      float cm = kNegInf;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if constexpr (KV == 8)
+          vm[u] = max2(max3(q[u].get(0), q[u].get(1), q[u].get(2)),
+                       max3(q[u].get(3), q[u].get(4), max3(q[u].get(5), q[u].get(6), q[u].get(7))));
+        else
+          vm[u] = max2(max3(q[u].get(0), q[u].get(1), q[u].get(2)), q[u].get(3));
+        cm = max2(cm, vm[u]);
       }
-      last = best;
+      // (unpacked again below: kept, the 32 values would cost half the waves)
+#pragma unroll
+      for (int u = 0; u < U; ++u) asm("" : "+v"(q[u].q[0]), "+v"(q[u].q[1]), "+v"(q[u].q[2]), "+v"(q[u].q[3]));
+      if (cm > ref + slack) {
+        move_to(cm, ref, c, s, w);
+        ref = rz = cm;
+      }
+      m = max2(m, cm);
+      if (TOP && vb == v0) {
+        // the wave's k-th largest lane maximum; its low bits give way to the
+        // lane, which only lowers it
+        const unsigned u = __float_as_uint((cm == cm ? cm : kNegInf) + 0.0f);
+        const unsigned key = (((u & 0x80000000u) ? ~u : (u | 0x80000000u)) & ~63u) | (63 - lane);
+        L.lane_max[tid] = key;
+        __syncthreads();
+        int rank = 0;
+#pragma unroll 16
+        for (int j = 0; j < 64; ++j) rank += L.lane_max[(tid & ~63) + j] > key;
+        const unsigned long long who = __ballot(rank == a.top - 1);
+        const unsigned kth = __builtin_amdgcn_readlane(key, __builtin_ctzll(who)) & ~63u;
+        if (lane == 0) L.wave_th[wave] = ordered_value(kth);
+        __syncthreads();
+        // (the cleared bits may have left a NaN below -inf's code)
+        th = kNegInf;
+        for (int i = 0; i < kWg / 64; ++i)
+          if (L.wave_th[i] > th) th = L.wave_th[i];
+        if (th > kNegInf) th = below(th);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (vb + u * kWg + wave * 64 >= v1) break;
+        const int v = vb + u * kWg + tid;
+        const float thr = v < tv ? ge : gt;
+        if (v == tv) {                                     // one lane of one chunk
+          for (int64_t j = (int64_t)v * KV; j < tok; ++j) ahead_lane += El::load(x[j]) == xt;
+        }
+#pragma unroll
+        for (int e = 0; e < KV; ++e) {
+          const float l = q[u].get(e), t = (l - rz) * c, ex = __builtin_amdgcn_exp2f(t);
+          s += ex;
+          w = fmaf(ex, max2(t, kLow), w);
+          ahead += __builtin_popcountll(__ballot(l > thr));
+        }
+        if (TOP && !(vm[u] <= th)) {
+#pragma unroll
+          for (int e = 0; e < KV; ++e) {
+            const float l = q[u].get(e);
+            if (l > th) {
+              const int at = pending + atomicAdd(&L.count[parity], 1) - seen[parity];
+              if (at < kCand) L.cand[at] = pack_key(l, static_cast<unsigned>(v) * KV + e);
+            }
+          }
+        }
+      }
+      if (TOP) {
+        __syncthreads();
+        const int got = L.count[parity] - seen[parity];
+        seen[parity] += got;
+        parity ^= 1;
+        if (pending + got > kCand) {
+          // more than there is room for (a row that rises, or is all equal):
+          // the chunk again, 256 candidates at a time
+          kcur = merge(L, cur, kcur, pending, a.top);
+          cur ^= 1;
+          const int64_t j0 = (int64_t)vb * KV, j1 = min(a.V, j0 + kWg * kChunk);
+          for (int64_t j = j0; j < j1; j += kWg) {
+            const unsigned long long least = kcur == a.top ? L.list[cur][kcur - 1] : 0ull;
+            if (j + tid < j1) {
+              const float l = El::load(x[j + tid]);
+              if (l > kNegInf) {
+                const unsigned long long key = pack_key(l, static_cast<unsigned>(j + tid));
+                if (key > least) L.cand[atomicAdd(&L.count[parity], 1) - seen[parity]] = key;
+              }
+            }
+            __syncthreads();
+            const int n = L.count[parity] - seen[parity];
+            seen[parity] += n;
+            parity ^= 1;
+            if (n > 0) {
+              kcur = merge(L, cur, kcur, n, a.top);
+              cur ^= 1;
+            }
+          }
+          pending = 0;
+          th = kcur == a.top ? key_value(L.list[cur][kcur - 1]) : kNegInf;
+        } else {
+          pending += got;
+          if (pending >= kMergeAt || vb + kWg * U >= v1) {
+            if (pending > 0) {
+              kcur = merge(L, cur, kcur, pending, a.top);
+              cur ^= 1;
+            }
+            pending = 0;
+            th = kcur == a.top ? key_value(L.list[cur][kcur - 1]) : kNegInf;
+          }
+        }
+      }
     }
+
+    // join the lanes
+    float M = wave_max(m);
+    if (lane == 0) fl[0][wave] = M;
+    __syncthreads();
+    for (int i = 0; i < kWg / 64; ++i) M = fmaxf(M, fl[0][i]);
+    move_to(M, ref, c, s, w);
+    s = wave_sum(s);
+    w = wave_sum(w);
+    int al = ahead_lane;
+    for (int off = 32; off > 0; off >>= 1) al += __shfl_xor(al, off);
+    if (lane == 0) {
+      fl[1][wave] = s;
+      fl[2][wave] = w;
+      il[wave] = ahead + al;
+    }
+    __syncthreads();
+    if (tid == 0) {
+      Partial p{M, fl[1][0], fl[2][0], il[0]};
+      for (int i = 1; i < kWg / 64; ++i) {
+        p.s += fl[1][i];
+        p.w += fl[2][i];
+        p.ahead += il[i];
+      }
+      if (splits == 1) row_ls = finish(a, row, p, tok, xt);
+      else static_cast<Partial*>(a.ws)[g] = p;
+    }
+    __syncthreads();
+    if (TOP && tid < a.top) {
+      const unsigned long long key = tid < kcur ? L.list[cur][tid] : 0ull;
+      if (splits == 1) {
+        finish_top(a, row, tid, key, M, row_ls);
+      } else {
+        unsigned long long* keys = reinterpret_cast<unsigned long long*>(static_cast<Partial*>(a.ws) + work);
+        keys[g * a.top + tid] = key;
+      }
+    }
+    __syncthreads();
+  }
+}
+
+constexpr int kMaxSplits = 64;
+constexpr int kMaxJoinKeys = 1024;
+
+// One workgroup per row joins its shares.
+template <int TYPE>
+__global__ __launch_bounds__(kWg) void k_logprobs_join(LogprobArgs a, int splits) {
+  using El = Elem<TYPE>;
+  __shared__ unsigned long long keys[kMaxJoinKeys];
+  __shared__ unsigned long long best[BO_MAX_ALTERNATIVES];
+  __shared__ float row_M, row_ls;
+  const int tid = threadIdx.x;
+  const float c = a.it * kLog2e;
+  for (int64_t row = blockIdx.x; row < a.T; row += gridDim.x) {
+    const Partial* ps = static_cast<const Partial*>(a.ws) + row * splits;
+    const unsigned long long* ks =
+        reinterpret_cast<const unsigned long long*>(static_cast<const Partial*>(a.ws) + a.T * splits) +
+        row * splits * a.top;
+    const int n = splits * a.top;
+    for (int i = tid; i < n; i += kWg) keys[i] = ks[i];
+    for (int i = tid; i < a.top; i += kWg) best[i] = 0ull;
+    if (tid < 64) {
+      Partial p{kNegInf, 0.0f, 0.0f, 0};
+      if (tid < splits) p = ps[tid];
+      const float M = wave_max(p.M);
+      move_to(M, p.M, c, p.s, p.w);
+      p.s = wave_sum(p.s);
+      p.w = wave_sum(p.w);
+      for (int off = 32; off > 0; off >>= 1) p.ahead += __shfl_xor(p.ahead, off);
+      p.M = M;
+      if (tid == 0) {
+        const typename El::T* x = static_cast<const typename El::T*>(a.logits) + row * a.stride;
+        const int64_t tok = a.tokens ? a.tokens[row] : -1;
+        const float xt = tok >= 0 && tok < a.V ? El::load(x[tok]) : 0.0f;
+        row_ls = finish(a, row, p, tok, xt);
+        row_M = M;
+      }
+    }
+    __syncthreads();
+    for (int i = tid; i < n; i += kWg) {
+      const unsigned long long key = keys[i];
+      int rank = 0;
+      for (int j = 0; j < n; ++j) rank += keys[j] > key;
+      if (key && rank < a.top) best[rank] = key;
+    }
+    __syncthreads();
+    if (tid < a.top) finish_top(a, row, tid, best[tid], row_M, row_ls);
     __syncthreads();
   }
 }
@@ -148,16 +415,43 @@ void by_type(int type, F32 f, BF16 b, F16 h) {
   else h();
 }
 
+// Shares of a row: enough workgroups for every compute unit when the rows are
+// few, whole chunks each.
+struct Split {
+  int splits, cps;
+};
+Split split_of(int64_t T, int64_t V, int top) {
+  const int64_t chunks = (V + kWg * kChunk - 1) / (kWg * kChunk);
+  int64_t want = T >= 1024 ? 1 : 1024 / T;
+  want = std::min<int64_t>({want, chunks, kMaxSplits, top > 0 ? kMaxJoinKeys / top : kMaxSplits});
+  const int64_t cps = (chunks + want - 1) / want;
+  return {static_cast<int>((chunks + cps - 1) / cps), static_cast<int>(cps)};
+}
+
+template <int TYPE>
+hipError_t launch(const LogprobArgs& a, hipStream_t st) {
+  const Split sp = split_of(a.T, a.V, a.top);
+  const int64_t work = a.T * sp.splits;
+  const dim3 grid(static_cast<unsigned>(std::min<int64_t>(work, 1 << 22)));
+  if (a.top > 0) k_logprobs<TYPE, true><<<grid, kWg, 0, st>>>(a, sp.splits, sp.cps);
+  else k_logprobs<TYPE, false><<<grid, kWg, 0, st>>>(a, sp.splits, sp.cps);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || sp.splits == 1) return e;
+  k_logprobs_join<TYPE><<<dim3(static_cast<unsigned>(a.T)), kWg, 0, st>>>(a, sp.splits);
+  return hipGetLastError();
+}
+
 }  // namespace
 
-int64_t logprob_workspace(int64_t, int64_t, int) { return 0; }
+int64_t logprob_workspace(int64_t T, int64_t V, int top) {
+  const Split sp = split_of(T, V, top);
+  return sp.splits == 1 ? 0 : T * sp.splits * static_cast<int64_t>(sizeof(Partial) + 8 * top);
+}
 
 hipError_t launch_logprobs(const LogprobArgs& a, hipStream_t st) {
-  const dim3 grid(static_cast<unsigned>(a.T < (1 << 20) ? a.T : (1 << 20)));
-  by_type(a.type, [&] { k_logprobs<BO_TYPE_F32><<<grid, kWg, 0, st>>>(a); },
-          [&] { k_logprobs<BO_TYPE_BF16><<<grid, kWg, 0, st>>>(a); },
-          [&] { k_logprobs<BO_TYPE_F16><<<grid, kWg, 0, st>>>(a); });
-  return hipGetLastError();
+  if (a.type == BO_TYPE_F32) return launch<BO_TYPE_F32>(a, st);
+  if (a.type == BO_TYPE_BF16) return launch<BO_TYPE_BF16>(a, st);
+  return launch<BO_TYPE_F16>(a, st);
 }
 
 hipError_t launch_logprobs_grad(const LogprobGradArgs& a, hipStream_t st) {

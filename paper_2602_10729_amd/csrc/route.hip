@@ -20,12 +20,6 @@ __device__ __forceinline__ float wave_sum(float v) {
   for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off);
   return v;
 }
-// Larger value first, the lower index among equals; 0 stands for none.
-__device__ __forceinline__ unsigned long long pack_key(float v, unsigned j) {
-  const unsigned u = __float_as_uint(v + 0.0f);
-  const unsigned o = (u & 0x80000000u) ? ~u : (u | 0x80000000u);
-  return (static_cast<unsigned long long>(o) << 32) | (0xFFFFFFFFu - j);
-}
 __device__ __forceinline__ unsigned long long wave_best(unsigned long long k) {
   for (int off = 32; off > 0; off >>= 1) {
     const unsigned long long o = __shfl_xor(k, off);

@@ -34,6 +34,82 @@ struct Elem<BO_TYPE_F16> {
   static __device__ __forceinline__ T store(float v) { return __float2half(v); }
 };
 
+// Sixteen bytes of logits in registers: kVec elements.
+template <int TYPE>
+struct Vec {
+  using T = typename Elem<TYPE>::T;
+  static constexpr int kVec = 16 / sizeof(T);
+  uint32_t q[4];
+  // Any alignment: rows start where their stride puts them, and the memory
+  // system takes a 16-byte access at every address.
+  __device__ __forceinline__ void load(const T* p) { __builtin_memcpy(q, p, 16); }
+  __device__ __forceinline__ void store(T* p) const { __builtin_memcpy(p, q, 16); }
+  // the first n elements, the rest -inf
+  __device__ __forceinline__ void load_part(const T* p, int n) {
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) set_bits(e, e < n ? bits_of(p[e]) : bits_of(Elem<TYPE>::store(-__builtin_huge_valf())));
+  }
+  __device__ __forceinline__ void store_part(T* p, int n) const {
+#pragma unroll
+    for (int e = 0; e < kVec; ++e)
+      if (e < n) {
+        if constexpr (kVec == 4) {
+          __builtin_memcpy(p + e, &q[e], 4);
+        } else {
+          const uint16_t h = static_cast<uint16_t>(q[e / 2] >> (16 * (e & 1)));
+          __builtin_memcpy(p + e, &h, 2);
+        }
+      }
+  }
+  __device__ __forceinline__ void fill_masked() {
+    const uint32_t b = bits_of(Elem<TYPE>::store(-__builtin_huge_valf()));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q[i] = kVec == 4 ? b : b | (b << 16);
+  }
+  __device__ __forceinline__ float get(int e) const {
+    if constexpr (TYPE == BO_TYPE_F32) return __uint_as_float(q[e]);
+    if constexpr (TYPE == BO_TYPE_BF16)
+      return __uint_as_float((e & 1) ? (q[e / 2] & 0xFFFF0000u) : (q[e / 2] << 16));
+    const uint16_t h = static_cast<uint16_t>(q[e / 2] >> (16 * (e & 1)));
+    _Float16 f;
+    __builtin_memcpy(&f, &h, 2);
+    return static_cast<float>(f);
+  }
+  __device__ __forceinline__ void set(int e, float v) { set_bits(e, bits_of(Elem<TYPE>::store(v))); }
+
+ private:
+  static __device__ __forceinline__ uint32_t bits_of(T v) {
+    if constexpr (kVec == 4) {
+      return __float_as_uint(v);
+    } else {
+      uint16_t h;
+      __builtin_memcpy(&h, &v, 2);
+      return h;
+    }
+  }
+  __device__ __forceinline__ void set_bits(int e, uint32_t b) {
+    if constexpr (kVec == 4) q[e] = b;
+    else q[e / 2] = (e & 1) ? (q[e / 2] & 0xFFFFu) | (b << 16) : (q[e / 2] & 0xFFFF0000u) | b;
+  }
+};
+
+// Larger value first, the lower index among equals, as the unsigned order of
+// one 64-bit key (-0 and +0 are equal); 0 is below every key of a value.
+__device__ __forceinline__ unsigned long long pack_key(float v, unsigned j) {
+  const unsigned u = __float_as_uint(v + 0.0f);
+  const unsigned o = (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+  return (static_cast<unsigned long long>(o) << 32) | (0xFFFFFFFFu - j);
+}
+__device__ __forceinline__ float ordered_value(unsigned o) {
+  return __uint_as_float((o & 0x80000000u) ? (o & 0x7FFFFFFFu) : ~o);
+}
+__device__ __forceinline__ float key_value(unsigned long long k) {
+  return ordered_value(static_cast<unsigned>(k >> 32));
+}
+__device__ __forceinline__ int key_index(unsigned long long k) {
+  return static_cast<int>(0xFFFFFFFFu - static_cast<unsigned>(k));
+}
+
 inline size_t type_bytes(int type) { return type == BO_TYPE_F32 ? 4 : 2; }
 
 struct LogprobArgs {
