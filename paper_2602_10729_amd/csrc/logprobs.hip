@@ -366,53 +366,94 @@ __global__ __launch_bounds__(kWg) void k_logprobs_join(LogprobArgs a, int splits
   }
 }
 
+// One workgroup per (row, share of the row's chunks): with t = c (l - m),
+//   grad_j = p_j (A + B u_j),  u_j = t - log2 s,  p_j = 2^u_j
+// streamed once, then the token's and the alternatives' terms put in place of
+// what the stream wrote there.
 template <int TYPE>
-__global__ __launch_bounds__(kWg) void k_logprobs_grad(LogprobGradArgs a) {
+__global__ __launch_bounds__(kWg) void k_logprobs_grad(LogprobGradArgs a, int splits, int cps) {
   using El = Elem<TYPE>;
-  __shared__ float onehot[BO_MAX_ALTERNATIVES + 1];
+  using V = Vec<TYPE>;
+  constexpr int KV = V::kVec, U = kChunk / KV;
+  __shared__ float hot[BO_MAX_ALTERNATIVES + 1];
   __shared__ int at[BO_MAX_ALTERNATIVES + 1];
-  for (int64_t row = blockIdx.x; row < a.T; row += gridDim.x) {
+  const int tid = threadIdx.x;
+  const int V_ = static_cast<int>(a.V), nv = (V_ - 1) / KV + 1;
+  const float c = a.it * kLog2e;
+  const int64_t work = a.T * splits;
+  for (int64_t g = blockIdx.x; g < work; g += gridDim.x) {
+    const int64_t row = splits == 1 ? g : g / splits;
+    const int part = splits == 1 ? 0 : static_cast<int>(g - row * splits);
     const typename El::T* x = static_cast<const typename El::T*>(a.logits) + row * a.stride;
     typename El::T* out = static_cast<typename El::T*>(a.out) + row * a.out_stride;
-    const float m = a.stats[2 * row], ls = a.stats[2 * row + 1];
+    const int v0 = min(nv, part * cps * (kWg * U)), v1 = min(nv, v0 + cps * (kWg * U));
+    const float m0 = a.stats[2 * row], ls0 = a.stats[2 * row + 1];
+    const bool empty = m0 == kNegInf && ls0 == kNegInf;
+    const float m = empty ? 0.0f : m0, ls2 = empty ? 0.0f : ls0 * kLog2e;
     const int64_t tok = a.tokens ? a.tokens[row] : -1;
     const bool has = tok >= 0 && tok < a.V;
     const float gl = has && a.g_logprob ? a.g_logprob[row] : 0.0f;
     const float gh = a.g_entropy ? a.g_entropy[row] : 0.0f;
-    float sum = gl;
-    for (int i = 0; i < a.top; ++i) {
-      const int id = a.top_ids[row * a.top + i];
-      if (id >= 0 && id < a.V) sum += a.g_top[row * a.top + i];
+    // this thread's one-hot term: alternative tid, or the token
+    int id = -1;
+    float own = 0.0f;
+    if (tid < a.top) {
+      id = a.top_ids[row * a.top + tid];
+      if (id < 0 || id >= V_) id = -1;
+      else own = a.g_top[row * a.top + tid];
+    } else if (tid == a.top && has) {
+      id = static_cast<int>(tok);
+      own = gl;
     }
-    __syncthreads();
-    for (int i = threadIdx.x; i <= a.top; i += kWg) {
-      const int64_t id = i < a.top ? a.top_ids[row * a.top + i] : (has ? tok : -1);
-      at[i] = id >= 0 && id < a.V ? static_cast<int>(id) : -1;
-      onehot[i] = i < a.top ? a.g_top[row * a.top + i] : gl;
+    if (tid <= a.top) {
+      at[tid] = id;
+      hot[tid] = own;
     }
+    if (id < v0 * (int64_t)KV || id >= v1 * (int64_t)KV || empty) id = -1;
+    const float xi = id >= 0 ? El::load(x[id]) : 0.0f;     // before the row may be overwritten
     __syncthreads();
-    const bool empty = m == kNegInf && ls == kNegInf;
-    float base = -sum - gh * a.entropy[row];
-    if (tok >= a.V) base = __builtin_nanf("");
-    for (int64_t j = threadIdx.x; j < a.V; j += kWg) {
-      float g = 0.0f;
-      if (!empty) {
-        const float u = (El::load(x[j]) - m) * a.it - ls;
-        g = exp2f(u * kLog2e) * (base - gh * fmaxf(u, kLow));
-        for (int i = 0; i <= a.top; ++i)
-          if (at[i] == j) g += onehot[i];
-        g *= a.it;
+    float total = 0.0f, mine = 0.0f;
+    for (int i = 0; i <= a.top; ++i) {
+      total += hot[i];
+      if (at[i] == id) mine += hot[i];
+    }
+    float A = a.it * (-total - gh * a.entropy[row]), B = -a.it * gh * kLn2;
+    if (tok >= a.V) A = __builtin_nanf("");
+    if (empty) A = B = 0.0f;
+    const auto grad = [&](float l) {
+      const float u = fmaf(l - m, c, -ls2);
+      return __builtin_amdgcn_exp2f(u) * fmaf(B, max2(u, kLow), A);
+    };
+    for (int vb = v0; vb < v1; vb += kWg * U) {
+      V q[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int v = vb + u * kWg + tid;
+        if (v < v1) {
+          const typename El::T* p = x + (int64_t)v * KV;
+          if (v < nv - 1 || V_ % KV == 0) q[u].load(p);
+          else q[u].load_part(p, V_ % KV);
+        }
       }
-      out[j] = El::store(g);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int v = vb + u * kWg + tid;
+        if (v < v1) {
+          float r[KV];
+#pragma unroll
+          for (int e = 0; e < KV; ++e) r[e] = grad(q[u].get(e));
+          q[u].set_all(r);
+          typename El::T* p = out + (int64_t)v * KV;
+          if (v < nv - 1 || V_ % KV == 0) q[u].store(p);
+          else q[u].store_part(p, V_ % KV);
+        }
+      }
     }
+    __syncthreads();
+    // (an id that is given twice has all its terms in each of its threads)
+    if (id >= 0) out[id] = El::store(grad(xi) + a.it * mine);
+    __syncthreads();
   }
-}
-
-template <typename F32, typename BF16, typename F16>
-void by_type(int type, F32 f, BF16 b, F16 h) {
-  if (type == BO_TYPE_F32) f();
-  else if (type == BO_TYPE_BF16) b();
-  else h();
 }
 
 // Shares of a row: enough workgroups for every compute unit when the rows are
@@ -455,10 +496,11 @@ hipError_t launch_logprobs(const LogprobArgs& a, hipStream_t st) {
 }
 
 hipError_t launch_logprobs_grad(const LogprobGradArgs& a, hipStream_t st) {
-  const dim3 grid(static_cast<unsigned>(a.T < (1 << 20) ? a.T : (1 << 20)));
-  by_type(a.type, [&] { k_logprobs_grad<BO_TYPE_F32><<<grid, kWg, 0, st>>>(a); },
-          [&] { k_logprobs_grad<BO_TYPE_BF16><<<grid, kWg, 0, st>>>(a); },
-          [&] { k_logprobs_grad<BO_TYPE_F16><<<grid, kWg, 0, st>>>(a); });
+  const Split sp = split_of(a.T, a.V, 0);
+  const dim3 grid(static_cast<unsigned>(std::min<int64_t>(a.T * sp.splits, 1 << 22)));
+  if (a.type == BO_TYPE_F32) k_logprobs_grad<BO_TYPE_F32><<<grid, kWg, 0, st>>>(a, sp.splits, sp.cps);
+  else if (a.type == BO_TYPE_BF16) k_logprobs_grad<BO_TYPE_BF16><<<grid, kWg, 0, st>>>(a, sp.splits, sp.cps);
+  else k_logprobs_grad<BO_TYPE_F16><<<grid, kWg, 0, st>>>(a, sp.splits, sp.cps);
   return hipGetLastError();
 }
 

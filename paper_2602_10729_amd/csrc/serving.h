@@ -2,8 +2,6 @@
 // (logprobs.hip), routing (route.hip) and dispatch (dispatch.hip).
 #pragma once
 
-#include <hip/hip_bf16.h>
-#include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -23,15 +21,15 @@ struct Elem<BO_TYPE_F32> {
 };
 template <>
 struct Elem<BO_TYPE_BF16> {
-  using T = __hip_bfloat16;
-  static __device__ __forceinline__ float load(T v) { return __bfloat162float(v); }
-  static __device__ __forceinline__ T store(float v) { return __float2bfloat16(v); }
+  using T = __bf16;
+  static __device__ __forceinline__ float load(T v) { return static_cast<float>(v); }
+  static __device__ __forceinline__ T store(float v) { return static_cast<__bf16>(v); }
 };
 template <>
 struct Elem<BO_TYPE_F16> {
-  using T = __half;
-  static __device__ __forceinline__ float load(T v) { return __half2float(v); }
-  static __device__ __forceinline__ T store(float v) { return __float2half(v); }
+  using T = _Float16;
+  static __device__ __forceinline__ float load(T v) { return static_cast<float>(v); }
+  static __device__ __forceinline__ T store(float v) { return static_cast<_Float16>(v); }
 };
 
 // Sixteen bytes of logits in registers: kVec elements.
@@ -75,7 +73,19 @@ struct Vec {
     __builtin_memcpy(&f, &h, 2);
     return static_cast<float>(f);
   }
-  __device__ __forceinline__ void set(int e, float v) { set_bits(e, bits_of(Elem<TYPE>::store(v))); }
+  // every element, each rounded once
+  __device__ __forceinline__ void set_all(const float (&v)[kVec]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (kVec == 4) {
+        q[i] = __float_as_uint(v[i]);
+      } else {
+        typedef T T2 __attribute__((ext_vector_type(2)));
+        const T2 h = {Elem<TYPE>::store(v[2 * i]), Elem<TYPE>::store(v[2 * i + 1])};
+        __builtin_memcpy(&q[i], &h, 4);
+      }
+    }
+  }
 
  private:
   static __device__ __forceinline__ uint32_t bits_of(T v) {
