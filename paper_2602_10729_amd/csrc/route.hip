@@ -1,8 +1,17 @@
 // Routing to experts: scores, the choice of groups and experts, weights, and
 // the gradient of the router's logits.
 //
-// One wave per row; lane l holds experts l, l + 64, ..; each choice is a
-// reduction of (value, lowest index) over the wave.
+// Choice: a row is held by `lpt` neighbouring lanes (a power of two up to 32),
+// each with 32 consecutive experts at most, so a wave takes 64 / lpt rows. An
+// expert is one 64-bit key, larger for a larger value and, among equals, for a
+// lower index: the value's order-preserving code and the index are the
+// mantissa of a double in [2^52, 2^53), so that keys compare and exchange with
+// one v_max_f64 and one v_min_f64, which this chip runs at the fp32 rate. A
+// lane sorts its experts by eights, keeping the K >= top best; lanes then
+// exchange lists by halves (the larger of a_i and b_{K-1-i} are the K best of
+// two falling lists, and form a bitonic sequence that log2 K steps sort).
+#include <algorithm>
+
 #include "serving.h"
 
 namespace bo {
@@ -10,7 +19,9 @@ namespace {
 
 constexpr int kWg = 256;
 constexpr float kNegInf = -__builtin_huge_valf();
-constexpr int kPerLane = BO_MAX_EXPERTS / 64;
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr int kSpan = 32;                    // experts a lane holds
+constexpr unsigned kExpTwo52 = 0x43300000u;  // high word of 2^52
 
 __device__ __forceinline__ float wave_max(float v) {
   for (int off = 32; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor(v, off));
@@ -20,116 +31,319 @@ __device__ __forceinline__ float wave_sum(float v) {
   for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off);
   return v;
 }
-__device__ __forceinline__ unsigned long long wave_best(unsigned long long k) {
-  for (int off = 32; off > 0; off >>= 1) {
-    const unsigned long long o = __shfl_xor(k, off);
-    k = o > k ? o : k;
-  }
-  return k;
-}
 __device__ __forceinline__ float sigmoid(float l) { return 1.0f / (1.0f + expf(-l)); }
 
-template <int TYPE>
-__global__ __launch_bounds__(kWg) void k_route(RouteArgs a) {
+// ---- keys -----------------------------------------------------------------
+// Exchanges go through LDS' swizzle, not DPP: a DPP read needs wait states
+// after the write, which the compiler does not know of behind inline assembly.
+template <int XOR>
+__device__ __forceinline__ int swap_lanes(int v) {
+  return __builtin_amdgcn_ds_swizzle(v, (XOR << 10) | 0x1F);
+}
+template <int XOR>
+__device__ __forceinline__ float swap_lanes(float v) {
+  return __int_as_float(swap_lanes<XOR>(__float_as_int(v)));
+}
+template <int XOR>
+__device__ __forceinline__ double swap_lanes(double v) {
+  return __hiloint2double(swap_lanes<XOR>(__double2hiint(v)), swap_lanes<XOR>(__double2loint(v)));
+}
+__device__ __forceinline__ double kmax(double a, double b) {
+  double d;
+  asm("v_max_f64 %0, %1, %2" : "=v"(d) : "v"(a), "v"(b));
+  return d;
+}
+__device__ __forceinline__ double kmin(double a, double b) {
+  double d;
+  asm("v_min_f64 %0, %1, %2" : "=v"(d) : "v"(a), "v"(b));
+  return d;
+}
+// the larger first
+__device__ __forceinline__ void order(double& a, double& b) {
+  const double hi = kmax(a, b), lo = kmin(a, b);
+  a = hi;
+  b = lo;
+}
+// A bitonic sequence into falling order.
+template <int N>
+__device__ __forceinline__ void bitonic(double* a) {
+#pragma unroll
+  for (int h = N / 2; h > 0; h >>= 1)
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if ((i & h) == 0) order(a[i], a[i + h]);
+}
+// Any sequence into falling order: halves, the second taken backwards.
+template <int N>
+__device__ __forceinline__ void sort(double* a) {
+  if constexpr (N > 1) {
+    sort<N / 2>(a);
+    sort<N / 2>(a + N / 2);
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) order(a[i], a[N - 1 - i]);
+    // both halves are bitonic, every key of the first above the second's
+    bitonic<N / 2>(a);
+    bitonic<N / 2>(a + N / 2);
+  }
+}
+// a: the K best of a and of the falling list b[0..NB), NB <= K.
+template <int K, int NB>
+__device__ __forceinline__ void keep_best(double* a, const double* b) {
+#pragma unroll
+  for (int i = 0; i < NB; ++i) a[K - 1 - i] = kmax(a[K - 1 - i], b[i]);
+  bitonic<K>(a);
+}
+
+// The value's order-preserving code (-0 as +0), and its key with the place
+// among the lane's experts. v is no NaN; -inf is none.
+__device__ __forceinline__ unsigned code_of(float v) {
+  const unsigned u = __float_as_uint(v + 0.0f);
+  return u ^ (static_cast<unsigned>(static_cast<int>(u) >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ double make_key(float v, int place) {
+  const unsigned o = code_of(v);
+  return __hiloint2double(static_cast<int>(kExpTwo52 | (o >> 12)),
+                          static_cast<int>((o << 20) | static_cast<unsigned>(kSpan - 1 - place)));
+}
+
+// (the code of -inf is 0x007FFFFF, the next one 0x00800000)
+__device__ __forceinline__ bool is_choice(double key) {
+  return static_cast<unsigned>(__double2hiint(key)) >= (kExpTwo52 | (0x00800000u >> 12));
+}
+
+// ---- reductions over a row's lanes ------------------------------------------
+template <typename F>
+__device__ __forceinline__ float row_reduce(float v, int lpt, F f) {
+  if (lpt > 1) v = f(v, swap_lanes<1>(v));
+  if (lpt > 2) v = f(v, swap_lanes<2>(v));
+  if (lpt > 4) v = f(v, swap_lanes<4>(v));
+  if (lpt > 8) v = f(v, swap_lanes<8>(v));
+  if (lpt > 16) v = f(v, swap_lanes<16>(v));
+  return v;
+}
+template <int K, int XOR>
+__device__ __forceinline__ void join_lists(double* a) {
+  double b[K];
+#pragma unroll
+  for (int i = 0; i < K; ++i) b[i] = swap_lanes<XOR>(a[i]);
+  keep_best<K, K>(a, b);
+}
+
+// Expert j's place in LDS: a gap after every 32 keeps lanes that walk groups of
+// 32 off one another's bank.
+__device__ __forceinline__ int at_of(int j) { return j + (j >> 5); }
+
+// 1 << shift lanes a row.
+template <int TYPE, int K, bool GROUPED>
+__global__ __launch_bounds__(kWg) void k_route(RouteArgs a, int shift) {
   using El = Elem<TYPE>;
-  __shared__ float value[kWg / 64][BO_MAX_EXPERTS];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  float* val = value[wave];
-  const int64_t rows = (int64_t)gridDim.x * (kWg / 64);
-  const int per = a.E / a.groups;
-  for (int64_t row0 = (int64_t)blockIdx.x * (kWg / 64); row0 < a.T; row0 += rows) {
-    const int64_t row = row0 + wave;
+  using V = Vec<TYPE>;
+  constexpr int kBlocks = kSpan / 8, kParts = 8 / V::kVec;
+  // a wave's rows: values and groups' codes; choices and what they weigh
+  __shared__ float lds_val[GROUPED ? kWg / 64 : 1][GROUPED ? 64 * (kSpan + 1) : 1];
+  __shared__ unsigned lds_grp[GROUPED ? kWg / 64 : 1][GROUPED ? 64 * kSpan / 2 : 1];
+  __shared__ int lds_id[kWg / 64][64 * K];
+  __shared__ float lds_w[kWg / 64][64 * K];
+  const auto fmax2 = [](float p, float q) { return fmaxf(p, q); };
+  const auto fadd2 = [](float p, float q) { return p + q; };
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lpt = 1 << shift, sub = lane & (lpt - 1), slot = lane >> shift, rows = 64 >> shift;
+  // experts a lane holds: whole eights, consecutive ones
+  const int span = ((((a.E + 7) >> 3) + lpt - 1) >> shift) << 3;
+  const int first = sub * span;
+  const int64_t step = (int64_t)gridDim.x * (kWg / 64) * rows;
+  for (int64_t base = ((int64_t)blockIdx.x * (kWg / 64) + wave) * rows; __syncthreads_or(base < a.T);
+       base += step) {
+    const int64_t row = base + slot;
     const bool live = row < a.T;
-    const typename El::T* x = static_cast<const typename El::T*>(a.logits) + (live ? row : 0) * a.stride;
-    // the softmax statistics (a NaN stays in the sum)
-    float m = kNegInf, sum = 1.0f;
+    const typename El::T* x =
+        static_cast<const typename El::T*>(a.logits) + (live ? row : 0) * a.stride;
+    V q[kBlocks * kParts];
+#pragma unroll
+    for (int p = 0; p < kBlocks * kParts; ++p) {
+      const int j = first + p * V::kVec;
+      if (p * V::kVec >= span || j >= a.E) q[p].fill_masked();
+      else if (j + V::kVec <= a.E) q[p].load(x + j);
+      else q[p].load_part(x + j, a.E - j);
+    }
+    const auto logit = [&](int i) { return q[i / V::kVec].get(i % V::kVec); };
+    // softmax statistics; a row with a NaN or +inf has no choice
+    float m = 0.0f, inv = 1.0f;
+    bool bad = false;
     if (a.score == BO_SCORE_SOFTMAX) {
-      for (int j = lane; j < a.E; j += 64) m = fmaxf(m, El::load(x[j]));
-      m = wave_max(m);
-      const float mr = m == kNegInf ? 0.0f : m;
-      sum = 0.0f;
-      for (int j = lane; j < a.E; j += 64) sum += expf(El::load(x[j]) - mr);
-      sum = wave_sum(sum);
+      m = kNegInf;
+#pragma unroll
+      for (int i = 0; i < kSpan; ++i) {
+        m = fmaxf(m, logit(i));
+        bad = bad || __builtin_isnan(logit(i));
+      }
+      m = row_reduce(m, lpt, fmax2);
+      bad = bad || m == __builtin_huge_valf();
+      bad = (__ballot(bad) >> (slot << shift) & (~0ull >> (64 - lpt))) != 0;
+      m = m == kNegInf ? 0.0f : m;
+      if (GROUPED || a.bias || !a.renorm) {
+        float t = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kSpan; ++i) t += __builtin_amdgcn_exp2f((logit(i) - m) * kLog2e);
+        inv = 1.0f / row_reduce(t, lpt, fadd2);
+      }
     }
-    const auto score = [&](float l) {
-      return a.score == BO_SCORE_SOFTMAX ? expf(l - (m == kNegInf ? 0.0f : m)) / sum : sigmoid(l);
+    const auto score = [&](float t) {
+      if (a.score == BO_SCORE_SIGMOID)
+        return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-t * kLog2e));
+      return __builtin_amdgcn_exp2f((t - m) * kLog2e) * inv;
     };
-    __syncthreads();
-    for (int j = lane; j < a.E; j += 64) {
-      const float l = El::load(x[j]), s = score(l), b = a.bias ? a.bias[j] : 0.0f;
-      float v = s + b;
-      if (!(l > kNegInf) || !(b > kNegInf) || !(v > kNegInf)) v = kNegInf;
-      val[j] = v;
-    }
-    __syncthreads();
-    // groups: each of the top_groups best in turn leaves its mark
-    unsigned long long kept[BO_MAX_EXPERTS / 64] = {};
-    if (a.groups > 1) {
-      unsigned long long gk[kPerLane];
-      for (int i = 0; i < kPerLane; ++i) {
-        gk[i] = 0;
-        const int g = lane + 64 * i;
-        if (g < a.groups) {
-          float b1 = kNegInf, b2 = kNegInf;
-          for (int e = 0; e < per; ++e) {
-            const float v = val[g * per + e];
-            b2 = fmaxf(b2, fminf(b1, v));
-            b1 = fmaxf(b1, v);
+    // what is compared, eight experts at a time; -inf where one cannot be chosen
+    const auto values = [&](int b, float (&v)[8]) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = logit(8 * b + e);
+      if (GROUPED || a.bias) {
+        if (a.score == BO_SCORE_SIGMOID) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            v[e] = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-v[e] * kLog2e));
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = __builtin_amdgcn_exp2f((v[e] - m) * kLog2e) * inv;
+        }
+        if (a.bias) {
+#pragma unroll
+          for (int p = 0; p < 2; ++p) {
+            Vec<BO_TYPE_F32> t;
+            const int j = first + 8 * b + 4 * p;
+            if (j >= a.E) t.fill_masked();
+            else if (j + 4 <= a.E) t.load(a.bias + j);
+            else t.load_part(a.bias + j, a.E - j);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[4 * p + e] += t.get(e);
           }
-          gk[i] = pack_key(a.group_best == 2 ? b1 + b2 : b1, g);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = logit(8 * b + e) > kNegInf ? v[e] : kNegInf;
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = fmaxf(v[e], kNegInf);     // a NaN is no choice
+    };
+    float* val = GROUPED ? lds_val[wave] + slot * lpt * (kSpan + 1) : nullptr;
+    if constexpr (GROUPED) {
+      const int per = a.E / a.groups;
+      unsigned* grp = lds_grp[wave] + slot * lpt * (kSpan / 2);
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b)
+        if (8 * b < span) {
+          float v[8];
+          values(b, v);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) val[at_of(first + 8 * b) + e] = v[e];
+        }
+      __syncthreads();
+      for (int g = sub; g < a.groups; g += lpt) {
+        float b1 = kNegInf, b2 = kNegInf;
+        for (int e = g * per; e < (g + 1) * per; ++e) {
+          const float t = val[at_of(e)];
+          b2 = fmaxf(b2, fminf(b1, t));
+          b1 = fmaxf(b1, t);
+        }
+        grp[g] = code_of(a.group_best == 2 ? b1 + b2 : b1);
+      }
+      __syncthreads();
+      // a group that top_groups or more come before is dropped
+      for (int g = sub; g < a.groups; g += lpt) {
+        const unsigned mine = grp[g];
+        int before = 0;
+        for (int o = 0; o < a.groups; ++o) before += grp[o] > mine || (grp[o] == mine && o < g);
+        if (before >= a.top_groups)
+          for (int e = g * per; e < (g + 1) * per; ++e) val[at_of(e)] = kNegInf;
+      }
+      __syncthreads();
+    }
+    // the lane's best
+    double best[K];
+    constexpr int B = K < 8 ? K : 8;
+#pragma unroll
+    for (int i = 0; i < K; ++i) best[i] = 0.0;
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b) {
+      if (8 * b < span) {
+        float v[8];
+        if constexpr (GROUPED) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            v[e] = val[at_of(first + 8 * b) + e];
+            if (!a.bias) v[e] = v[e] > kNegInf ? logit(8 * b + e) : kNegInf;
+          }
+        } else {
+          values(b, v);
+        }
+#pragma unroll
+        for (int p = 0; p < 8 / B; ++p) {
+          double key[B];
+#pragma unroll
+          for (int e = 0; e < B; ++e) key[e] = make_key(v[p * B + e], 8 * b + p * B + e);
+          sort<B>(key);
+          if (b == 0 && p == 0) {
+#pragma unroll
+            for (int e = 0; e < B; ++e) best[e] = key[e];
+          } else {
+            keep_best<K, B>(best, key);
+          }
         }
       }
-      for (int n = 0; n < a.top_groups; ++n) {
-        unsigned long long best = 0;
-        for (int i = 0; i < kPerLane; ++i) best = gk[i] > best ? gk[i] : best;
-        best = wave_best(best);
-        const unsigned g = 0xFFFFFFFFu - static_cast<unsigned>(best);
-        for (int i = 0; i < kPerLane; ++i) {
-          if (gk[i] == best) gk[i] = 0;
-          if (static_cast<int>(g >> 6) == i) kept[i] |= 1ull << (g & 63);
-        }
+    }
+    // the row's best: the lane joins the key
+#pragma unroll
+    for (int i = 0; i < K; ++i)
+      best[i] = __hiloint2double(__double2hiint(best[i]),
+                                 __double2loint(best[i]) | ((31 - sub) << 5));
+    if (lpt > 1) join_lists<K, 1>(best);
+    if (lpt > 2) join_lists<K, 2>(best);
+    if (lpt > 4) join_lists<K, 4>(best);
+    if (lpt > 8) join_lists<K, 8>(best);
+    if (lpt > 16) join_lists<K, 16>(best);
+    // weights: lane `sub` takes choices sub, sub + lpt, ..
+    int* cid = lds_id[wave] + slot * K;
+    float* cw = lds_w[wave] + slot * K;
+    if (sub == 0) {
+#pragma unroll
+      for (int i = 0; i < K; ++i) {
+        const int lo = __double2loint(best[i]);
+        cid[i] = is_choice(best[i]) && !bad ? (31 - ((lo >> 5) & 31)) * span + (kSpan - 1 - (lo & 31)) : -1;
       }
     }
-    unsigned long long key[kPerLane];
-    for (int i = 0; i < kPerLane; ++i) {
-      const int j = lane + 64 * i;
-      key[i] = 0;
-      if (j < a.E && val[j] > kNegInf) {
-        const float v = a.bias ? val[j] : El::load(x[j]);
-        const int g = j / per;
-        bool in = a.groups == 1;
-        for (int q = 0; q < kPerLane; ++q)
-          if ((g >> 6) == q) in = in || ((kept[q] >> (g & 63)) & 1);
-        if (in) key[i] = pack_key(v, j);
-      }
+    __syncthreads();
+    float hi = kNegInf, total = 0.0f, norm = 1.0f;
+    for (int n = sub; n < a.top; n += lpt) {
+      const int id = cid[n];
+      const float t = id >= 0 ? El::load(x[id]) : kNegInf;
+      hi = fmaxf(hi, t);
+      cw[n] = t;
     }
-    int mine = -1;
-    for (int n = 0; n < a.top; ++n) {
-      unsigned long long best = 0;
-      for (int i = 0; i < kPerLane; ++i) best = key[i] > best ? key[i] : best;
-      best = wave_best(best);
-      for (int i = 0; i < kPerLane; ++i)
-        if (key[i] == best) key[i] = 0;
-      if (lane == n && best) mine = static_cast<int>(0xFFFFFFFFu - static_cast<unsigned>(best));
-    }
-    // weights: lane n holds choice n; relative to the largest chosen logit
-    // where they are renormalised
-    const float l = mine >= 0 ? El::load(x[mine]) : kNegInf;
-    float w = 0.0f;
     if (a.renorm) {
-      float top = wave_max(l);
-      if (a.score == BO_SCORE_SIGMOID) top = fminf(top, 0.0f);
-      if (mine >= 0) w = a.score == BO_SCORE_SOFTMAX ? expf(l - top)
-                         : l > 0.0f ? sigmoid(l) : expf(l - top) / (1.0f + expf(l));
-      const float total = wave_sum(w);
-      if (mine >= 0) w = w / total;
-    } else if (mine >= 0) {
-      w = score(l);
+      // relative to the largest chosen score, so that none underflows
+      hi = row_reduce(hi, lpt, fmax2);
+      if (a.score == BO_SCORE_SIGMOID) hi = fminf(hi, 0.0f);
     }
-    if (live && lane < a.top) {
-      a.ids[row * a.top + lane] = mine;
-      a.weights[row * a.top + lane] = a.scale * w;
+    for (int n = sub; n < a.top; n += lpt) {
+      const float t = cw[n];
+      float w;
+      if (!a.renorm || (a.score == BO_SCORE_SIGMOID && t > 0.0f)) w = score(t);
+      else w = __builtin_amdgcn_exp2f((t - hi) * kLog2e);
+      if (a.renorm && a.score == BO_SCORE_SIGMOID && !(t > 0.0f))
+        w *= __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(t * kLog2e));
+      w = cid[n] >= 0 ? w : 0.0f;
+      cw[n] = w;
+      total += w;
     }
+    if (a.renorm) {
+      total = row_reduce(total, lpt, fadd2);
+      norm = total > 0.0f ? 1.0f / total : 0.0f;
+    }
+    if (live)
+      for (int n = sub; n < a.top; n += lpt) {
+        a.ids[row * a.top + n] = cid[n];
+        a.weights[row * a.top + n] = a.scale * (cw[n] * norm);
+      }
+    __syncthreads();
   }
 }
 
@@ -185,6 +399,27 @@ __global__ __launch_bounds__(kWg) void k_route_grad(RouteGradArgs a) {
   }
 }
 
+template <int TYPE, int K>
+void launch_choice(const RouteArgs& a, int shift, unsigned grid, hipStream_t st) {
+  if (a.groups > 1 && a.top_groups < a.groups) k_route<TYPE, K, true><<<grid, kWg, 0, st>>>(a, shift);
+  else k_route<TYPE, K, false><<<grid, kWg, 0, st>>>(a, shift);
+}
+
+template <int TYPE>
+hipError_t launch_typed(const RouteArgs& a, hipStream_t st) {
+  // as few lanes a row as hold it
+  int shift = 0;
+  while ((kSpan << shift) < a.E) ++shift;
+  const int64_t rows = (64 >> shift) * (kWg / 64);
+  const unsigned grid = static_cast<unsigned>(std::min<int64_t>((a.T + rows - 1) / rows, 1 << 20));
+  if (a.top <= 2) launch_choice<TYPE, 2>(a, shift, grid, st);
+  else if (a.top <= 4) launch_choice<TYPE, 4>(a, shift, grid, st);
+  else if (a.top <= 8) launch_choice<TYPE, 8>(a, shift, grid, st);
+  else if (a.top <= 16) launch_choice<TYPE, 16>(a, shift, grid, st);
+  else launch_choice<TYPE, 32>(a, shift, grid, st);
+  return hipGetLastError();
+}
+
 template <typename F32, typename BF16, typename F16>
 void by_type(int type, F32 f, BF16 b, F16 h) {
   if (type == BO_TYPE_F32) f();
@@ -200,11 +435,9 @@ unsigned row_blocks(int64_t T) {
 }  // namespace
 
 hipError_t launch_route(const RouteArgs& a, hipStream_t st) {
-  const dim3 grid(row_blocks(a.T));
-  by_type(a.type, [&] { k_route<BO_TYPE_F32><<<grid, kWg, 0, st>>>(a); },
-          [&] { k_route<BO_TYPE_BF16><<<grid, kWg, 0, st>>>(a); },
-          [&] { k_route<BO_TYPE_F16><<<grid, kWg, 0, st>>>(a); });
-  return hipGetLastError();
+  if (a.type == BO_TYPE_F32) return launch_typed<BO_TYPE_F32>(a, st);
+  if (a.type == BO_TYPE_BF16) return launch_typed<BO_TYPE_BF16>(a, st);
+  return launch_typed<BO_TYPE_F16>(a, st);
 }
 
 hipError_t launch_route_grad(const RouteGradArgs& a, hipStream_t st) {

@@ -42,10 +42,14 @@ struct Vec {
   // system takes a 16-byte access at every address.
   __device__ __forceinline__ void load(const T* p) { __builtin_memcpy(q, p, 16); }
   __device__ __forceinline__ void store(T* p) const { __builtin_memcpy(p, q, 16); }
-  // the first n elements, the rest -inf
+  // the first n >= 1 elements, the rest -inf (the first one read again)
   __device__ __forceinline__ void load_part(const T* p, int n) {
+    const uint32_t none = bits_of(Elem<TYPE>::store(-__builtin_huge_valf()));
 #pragma unroll
-    for (int e = 0; e < kVec; ++e) set_bits(e, e < n ? bits_of(p[e]) : bits_of(Elem<TYPE>::store(-__builtin_huge_valf())));
+    for (int e = 0; e < kVec; ++e) {
+      const uint32_t b = bits_of(p[e < n ? e : 0]);
+      set_bits(e, e < n ? b : none);
+    }
   }
   __device__ __forceinline__ void store_part(T* p, int n) const {
 #pragma unroll
