@@ -23,16 +23,6 @@ constexpr float kLog2e = 1.44269504088896340736f;
 constexpr int kSpan = 32;                    // experts a lane holds
 constexpr unsigned kExpTwo52 = 0x43300000u;  // high word of 2^52
 
-__device__ __forceinline__ float wave_max(float v) {
-  for (int off = 32; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor(v, off));
-  return v;
-}
-__device__ __forceinline__ float wave_sum(float v) {
-  for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off);
-  return v;
-}
-__device__ __forceinline__ float sigmoid(float l) { return 1.0f / (1.0f + expf(-l)); }
-
 // ---- keys -----------------------------------------------------------------
 // Exchanges go through LDS' swizzle, not DPP: a DPP read needs wait states
 // after the write, which the compiler does not know of behind inline assembly.
@@ -152,9 +142,8 @@ __global__ __launch_bounds__(kWg) void k_route(RouteArgs a, int shift) {
   const int span = ((((a.E + 7) >> 3) + lpt - 1) >> shift) << 3;
   const int first = sub * span;
   const int64_t step = (int64_t)gridDim.x * (kWg / 64) * rows;
-  for (int64_t base = ((int64_t)blockIdx.x * (kWg / 64) + wave) * rows; __syncthreads_or(base < a.T);
-       base += step) {
-    const int64_t row = base + slot;
+  for (int64_t base = (int64_t)blockIdx.x * (kWg / 64) * rows; base < a.T; base += step) {
+    const int64_t row = base + wave * rows + slot;
     const bool live = row < a.T;
     const typename El::T* x =
         static_cast<const typename El::T*>(a.logits) + (live ? row : 0) * a.stride;
@@ -347,56 +336,131 @@ __global__ __launch_bounds__(kWg) void k_route(RouteArgs a, int shift) {
   }
 }
 
+// The same lanes hold a row: each choice's term goes to its expert's place in
+// LDS, then every lane adds the dense part (softmax, not renormalised: -scale
+// s_j sum_k s_k g_k) to its experts' and writes them.
 template <int TYPE>
-__global__ __launch_bounds__(kWg) void k_route_grad(RouteGradArgs a) {
+__global__ __launch_bounds__(kWg) void k_route_grad(RouteGradArgs a, int shift) {
   using El = Elem<TYPE>;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t rows = (int64_t)gridDim.x * (kWg / 64);
-  for (int64_t row = (int64_t)blockIdx.x * (kWg / 64) + wave; row < a.T; row += rows) {
-    const typename El::T* x = static_cast<const typename El::T*>(a.logits) + row * a.stride;
-    typename El::T* out = static_cast<typename El::T*>(a.out) + row * a.out_stride;
-    int id = lane < a.top ? a.ids[row * a.top + lane] : -1;
-    if (id >= a.E) id = -1;
-    const bool on = id >= 0;
-    const float g = on ? a.g[row * a.top + lane] : 0.0f;
-    const float l = on ? El::load(x[id]) : kNegInf;
-    const bool any = __ballot(on) != 0;
-    float m = kNegInf, sum = 1.0f, s = 0.0f, w = 0.0f, inner = 0.0f, d = 0.0f;
-    if (any && a.renorm) {
-      float top = wave_max(l);
-      if (a.score == BO_SCORE_SIGMOID) top = fminf(top, 0.0f);
-      if (on) w = a.score == BO_SCORE_SOFTMAX ? expf(l - top)
-                  : l > 0.0f ? sigmoid(l) : expf(l - top) / (1.0f + expf(l));
-      const float total = wave_sum(w);
-      if (on) w = w / total;
-      const float mean = wave_sum(w * g);
-      d = on ? a.scale * w * (g - mean) : 0.0f;
-      if (on && a.score == BO_SCORE_SIGMOID) d *= sigmoid(-l);
-    } else if (any && a.score == BO_SCORE_SIGMOID) {
-      d = on ? a.scale * g * sigmoid(l) * sigmoid(-l) : 0.0f;
-    } else if (any) {
-      for (int j = lane; j < a.E; j += 64) m = fmaxf(m, El::load(x[j]));
-      m = wave_max(m);
-      sum = 0.0f;
-      for (int j = lane; j < a.E; j += 64) sum += expf(El::load(x[j]) - m);
-      sum = wave_sum(sum);
-      s = on ? expf(l - m) / sum : 0.0f;
-      inner = wave_sum(s * g);
-      d = a.scale * s * g;
-    }
-    const bool dense = any && !a.renorm && a.score == BO_SCORE_SOFTMAX;
-    for (int j0 = 0; j0 < a.E; j0 += 64) {
-      const int j = j0 + lane;
-      float v = 0.0f;
-      if (dense && j < a.E) v = -a.scale * inner * (expf(El::load(x[j]) - m) / sum);
-      for (int n = 0; n < a.top; ++n) {
-        const int at = __shfl(id, n);
-        const float dn = __shfl(d, n);
-        if (at == j) v += dn;
+  using V = Vec<TYPE>;
+  constexpr int kParts = kSpan / V::kVec;
+  __shared__ float lds_term[kWg / 64][64 * (kSpan + 1)];
+  const auto fmax2 = [](float p, float q) { return fmaxf(p, q); };
+  const auto fadd2 = [](float p, float q) { return p + q; };
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lpt = 1 << shift, sub = lane & (lpt - 1), slot = lane >> shift, rows = 64 >> shift;
+  const int span = ((((a.E + 7) >> 3) + lpt - 1) >> shift) << 3;
+  const int first = sub * span;
+  const int64_t step = (int64_t)gridDim.x * (kWg / 64) * rows;
+  const bool softmax = a.score == BO_SCORE_SOFTMAX, dense = softmax && !a.renorm;
+  float* term = lds_term[wave] + slot * lpt * (kSpan + 1);
+  for (int64_t base = (int64_t)blockIdx.x * (kWg / 64) * rows; base < a.T; base += step) {
+    const int64_t row = base + wave * rows + slot;
+    const bool live = row < a.T;
+    const int64_t r = live ? row : 0;
+    const typename El::T* x = static_cast<const typename El::T*>(a.logits) + r * a.stride;
+    const int32_t* ids = a.ids + r * a.top;
+    const float* g = a.g + r * a.top;
+    V q[kParts];
+    float m = 0.0f, inv = 1.0f;
+    if (dense) {
+#pragma unroll
+      for (int p = 0; p < kParts; ++p) {
+        const int j = first + p * V::kVec;
+        if (p * V::kVec >= span || j >= a.E) q[p].fill_masked();
+        else if (j + V::kVec <= a.E) q[p].load(x + j);
+        else q[p].load_part(x + j, a.E - j);
       }
-      if (j < a.E) out[j] = El::store(v);
+      m = kNegInf;
+#pragma unroll
+      for (int i = 0; i < kSpan; ++i) m = fmaxf(m, q[i / V::kVec].get(i % V::kVec));
+      m = row_reduce(m, lpt, fmax2);
+      m = m == kNegInf ? 0.0f : m;
+      float t = 0.0f;
+#pragma unroll
+      for (int i = 0; i < kSpan; ++i)
+        t += __builtin_amdgcn_exp2f((q[i / V::kVec].get(i % V::kVec) - m) * kLog2e);
+      inv = 1.0f / row_reduce(t, lpt, fadd2);
     }
+#pragma unroll
+    for (int b = 0; b < kSpan / 8; ++b)
+      if (8 * b < span) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) term[at_of(first + 8 * b) + e] = 0.0f;
+      }
+    __syncthreads();
+    const auto sigm = [](float t) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-t * kLog2e)); };
+    float hi = kNegInf, any = 0.0f;
+    for (int n = sub; n < a.top; n += lpt) {
+      const int id = ids[n];
+      if (id >= 0 && id < a.E) {
+        hi = fmaxf(hi, El::load(x[id]));
+        any = 1.0f;
+      }
+    }
+    any = row_reduce(any, lpt, fmax2);
+    hi = row_reduce(hi, lpt, fmax2);
+    if (!softmax) hi = fminf(hi, 0.0f);
+    // the weights before their common factor, as in the forward pass
+    const auto weight = [&](float l) {
+      if (dense) return __builtin_amdgcn_exp2f((l - m) * kLog2e) * inv;
+      if (!a.renorm) return sigm(l);
+      if (!softmax && l > 0.0f) return sigm(l);
+      const float w = __builtin_amdgcn_exp2f((l - hi) * kLog2e);
+      return softmax ? w : w * sigm(-l);
+    };
+    float total = 0.0f, wg = 0.0f;
+    for (int n = sub; n < a.top; n += lpt) {
+      const int id = ids[n];
+      if (id >= 0 && id < a.E) {
+        const float w = weight(El::load(x[id]));
+        total += w;
+        wg = fmaf(w, g[n], wg);
+      }
+    }
+    total = row_reduce(total, lpt, fadd2);
+    wg = row_reduce(wg, lpt, fadd2);
+    const float norm = a.renorm ? 1.0f / total : 1.0f, mean = a.renorm ? wg * norm : 0.0f;
+    for (int n = sub; n < a.top; n += lpt) {
+      const int id = ids[n];
+      if (id >= 0 && id < a.E) {
+        const float l = El::load(x[id]);
+        float d = a.scale * (weight(l) * norm) * (g[n] - mean);
+        if (!softmax) d *= sigm(-l);
+        term[at_of(id)] = d;
+      }
+    }
+    __syncthreads();
+    typename El::T* out = static_cast<typename El::T*>(a.out) + r * a.out_stride;
+    const float back = dense && any > 0.0f ? -a.scale * wg * inv : 0.0f;
+#pragma unroll
+    for (int p = 0; p < kParts; ++p) {
+      const int j = first + p * V::kVec;
+      if (p * V::kVec < span && j < a.E && live) {
+        float v[V::kVec];
+#pragma unroll
+        for (int e = 0; e < V::kVec; ++e) {
+          v[e] = term[at_of(j) + e];
+          if (back != 0.0f) v[e] = fmaf(back, __builtin_amdgcn_exp2f((q[p].get(e) - m) * kLog2e), v[e]);
+        }
+        q[p].set_all(v);
+        if (j + V::kVec <= a.E) q[p].store(out + j);
+        else q[p].store_part(out + j, a.E - j);
+      }
+    }
+    __syncthreads();
   }
+}
+
+// As few lanes a row as hold it.
+int lanes_shift(int E) {
+  int shift = 0;
+  while ((kSpan << shift) < E) ++shift;
+  return shift;
+}
+unsigned row_blocks(int64_t T, int shift) {
+  const int64_t rows = (64 >> shift) * (kWg / 64);
+  return static_cast<unsigned>(std::min<int64_t>((T + rows - 1) / rows, 1 << 20));
 }
 
 template <int TYPE, int K>
@@ -407,29 +471,14 @@ void launch_choice(const RouteArgs& a, int shift, unsigned grid, hipStream_t st)
 
 template <int TYPE>
 hipError_t launch_typed(const RouteArgs& a, hipStream_t st) {
-  // as few lanes a row as hold it
-  int shift = 0;
-  while ((kSpan << shift) < a.E) ++shift;
-  const int64_t rows = (64 >> shift) * (kWg / 64);
-  const unsigned grid = static_cast<unsigned>(std::min<int64_t>((a.T + rows - 1) / rows, 1 << 20));
+  const int shift = lanes_shift(a.E);
+  const unsigned grid = row_blocks(a.T, shift);
   if (a.top <= 2) launch_choice<TYPE, 2>(a, shift, grid, st);
   else if (a.top <= 4) launch_choice<TYPE, 4>(a, shift, grid, st);
   else if (a.top <= 8) launch_choice<TYPE, 8>(a, shift, grid, st);
   else if (a.top <= 16) launch_choice<TYPE, 16>(a, shift, grid, st);
   else launch_choice<TYPE, 32>(a, shift, grid, st);
   return hipGetLastError();
-}
-
-template <typename F32, typename BF16, typename F16>
-void by_type(int type, F32 f, BF16 b, F16 h) {
-  if (type == BO_TYPE_F32) f();
-  else if (type == BO_TYPE_BF16) b();
-  else h();
-}
-
-unsigned row_blocks(int64_t T) {
-  const int64_t b = (T + kWg / 64 - 1) / (kWg / 64);
-  return static_cast<unsigned>(b < (1 << 20) ? b : (1 << 20));
 }
 
 }  // namespace
@@ -441,10 +490,11 @@ hipError_t launch_route(const RouteArgs& a, hipStream_t st) {
 }
 
 hipError_t launch_route_grad(const RouteGradArgs& a, hipStream_t st) {
-  const dim3 grid(row_blocks(a.T));
-  by_type(a.type, [&] { k_route_grad<BO_TYPE_F32><<<grid, kWg, 0, st>>>(a); },
-          [&] { k_route_grad<BO_TYPE_BF16><<<grid, kWg, 0, st>>>(a); },
-          [&] { k_route_grad<BO_TYPE_F16><<<grid, kWg, 0, st>>>(a); });
+  const int shift = lanes_shift(a.E);
+  const unsigned grid = row_blocks(a.T, shift);
+  if (a.type == BO_TYPE_F32) k_route_grad<BO_TYPE_F32><<<grid, kWg, 0, st>>>(a, shift);
+  else if (a.type == BO_TYPE_BF16) k_route_grad<BO_TYPE_BF16><<<grid, kWg, 0, st>>>(a, shift);
+  else k_route_grad<BO_TYPE_F16><<<grid, kWg, 0, st>>>(a, shift);
   return hipGetLastError();
 }
 
