@@ -1,11 +1,14 @@
 // Log probabilities of given tokens, entropy, ranks and alternatives, and the
 // gradient of the logits.
 //
-// Forward, one pass over a row: a lane keeps a reference r near its largest
-// logit, s = sum exp2(t) and w = sum t exp2(t) with t = c (l - r), c =
-// log2(e) / temperature; lanes are joined by moving their sums to the row's
-// maximum M:
-//   s' = s 2^d,  w' = (w + d s) 2^d,  d = c (r - M).
+// Forward, one pass over a row, in powers of two: with c = log2(e) /
+// temperature, a lane keeps a reference r near its largest logit, R = c r
+// rounded, s = sum 2^t and w = sum t 2^t with t = c l - R (one fma). Lanes are
+// joined by moving their sums to the row's maximum M:
+//   s' = s 2^d,  w' = (w + d s) 2^d,  d = R - R_M;
+// what R_M lost in rounding, c M - R_M, goes back into the logarithm of the
+// sum. A masked logit makes t 2^t NaN: a chunk that ends with w not finite is
+// summed again with t bounded from below, and the wave stays on that path.
 // The largest logits are collected on the way: a workgroup knows a threshold
 // that at least `top` logits of the row reach, appends what lies above it to a
 // list in LDS, and now and then keeps the list's `top` best, whose last raises
@@ -13,6 +16,7 @@
 // appended falls off with the place in the row, about top / chunk number a
 // chunk, so the search costs one comparison of a vector's maximum.
 #include <algorithm>
+#include <type_traits>
 
 #include "serving.h"
 
@@ -25,12 +29,15 @@ constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
 // A finite stand-in for -inf where it is multiplied by a probability of 0.
 constexpr float kLow = -1e30f;
-constexpr int kChunk = 32;               // elements a thread holds at once
+constexpr int kVecs = 4;                 // vectors a thread holds at once (16 bytes each)
+constexpr int kUnit = 8192;              // elements by which a row is shared out
 constexpr int kCand = 768;               // room for appended candidates
 constexpr int kMergeAt = 32;             // candidates that are worth a merge
 // A lane's reference follows its maximum when that is this far above (in
-// powers of two): exp2 stays below 2^4 and few chunks pay for a rescale.
-constexpr float kSlack = 4.0f;
+// powers of two). A wave pays for the move when one of its lanes makes it: at 4
+// most vectors did (logits a few units wide), which took as many instructions
+// as the sums. The entropy loses 16 units of its last place at most.
+constexpr float kSlack = 16.0f;
 
 // max of three; NaN operands are dropped (a signalling one may come through)
 __device__ __forceinline__ float max3(float a, float b, float c) {
@@ -51,23 +58,48 @@ __device__ __forceinline__ float below(float v) {
   return __uint_as_float(v > 0.0f ? u - 1 : u + 1);
 }
 
+// Reductions over the wave by DPP: rows of 16 by shifts, then across rows; the
+// last lane holds the result, which is given to all. The order is fixed.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float dpp(float none, float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(none), __float_as_int(v), CTRL, ROWS, 0xF, false));
+}
+template <typename F>
+__device__ __forceinline__ float wave_reduce(float v, float none, F f) {
+  v = f(v, dpp<0x111, 0xF>(none, v));
+  v = f(v, dpp<0x112, 0xF>(none, v));
+  v = f(v, dpp<0x114, 0xF>(none, v));
+  v = f(v, dpp<0x118, 0xF>(none, v));
+  v = f(v, dpp<0x142, 0xA>(none, v));
+  v = f(v, dpp<0x143, 0xC>(none, v));
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
 __device__ __forceinline__ float wave_max(float v) {
-  for (int off = 32; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor(v, off));
-  return v;
+  return wave_reduce(v, kNegInf, [](float p, float q) { return fmaxf(p, q); });
 }
 __device__ __forceinline__ float wave_sum(float v) {
-  for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off);
-  return v;
+  return wave_reduce(v, 0.0f, [](float p, float q) { return p + q; });
 }
 
+// References this large (the type's lowest value) leave fp32 when scaled.
+constexpr float kFar = 1e37f;
+// (Rounded by itself: contracted into what uses it, the lanes' references would
+// no longer be the ones that their sums are relative to.)
+__device__ __forceinline__ float scaled_ref(float r, float c) {
+#pragma clang fp contract(off)
+  return fabsf(r) < kFar ? r * c : 0.0f;
+}
 // (s, w) relative to r, moved to M >= r: a lane without a finite logit has
 // r = -inf and s = 0 (or NaN, which stays).
 __device__ __forceinline__ void move_to(float M, float r, float c, float& s, float& w) {
+#pragma clang fp contract(off)
   if (r == kNegInf) return;
-  const float d = fmaxf((r - M) * c, kLow), f = __builtin_amdgcn_exp2f(d);
+  float d = scaled_ref(r, c) - scaled_ref(M, c);
+  if (!(fabsf(r) < kFar && fabsf(M) < kFar)) d = fmaxf((r - M) * c, kLow);
+  const float f = __builtin_amdgcn_exp2f(d);
   w = (w + s * d) * f;
   s *= f;
-  if (r != r || M - M != 0.0f) s = w = __builtin_nanf("");
+  if (M - M != 0.0f) s = w = __builtin_nanf("");
 }
 
 struct Partial {      // of one row's share
@@ -79,10 +111,12 @@ struct Partial {      // of one row's share
 __device__ __forceinline__ float finish(const LogprobArgs& a, int64_t row, const Partial& p,
                                         int64_t tok, float xt) {
   const bool has = tok >= 0 && tok < a.V;
-  const float ls = logf(p.s);
+  const float c = a.it * kLog2e;
+  const float lost = fabsf(p.M) < kFar ? fmaf(p.M, c, -scaled_ref(p.M, c)) : 0.0f;
+  const float ls0 = logf(p.s), ls = ls0 - lost * kLn2;
   a.stats[2 * row] = p.M;
   a.stats[2 * row + 1] = ls;
-  a.entropy[row] = p.M == kNegInf && p.s == 0.0f ? 0.0f : ls - p.w / p.s * kLn2;
+  a.entropy[row] = p.M == kNegInf && p.s == 0.0f ? 0.0f : ls0 - p.w / p.s * kLn2;
   float lp = 0.0f;
   if (has) lp = xt == kNegInf && p.s == p.s ? kNegInf : (xt - p.M) * a.it - ls;
   if (tok >= a.V) lp = __builtin_nanf("");
@@ -96,13 +130,27 @@ __device__ __forceinline__ void finish_top(const LogprobArgs& a, int64_t row, in
   a.top_logprobs[row * a.top + i] = key ? (key_value(key) - M) * a.it - ls : kNegInf;
 }
 
-struct TopLds {
+struct alignas(16) TopLds {
   unsigned long long list[2][BO_MAX_ALTERNATIVES];
-  unsigned long long cand[kCand];
+  unsigned long long cand[kCand + 2];
   unsigned lane_max[kWg];
   float wave_th[kWg / 64];
   int count[2];
 };
+
+// How many of keys[0..n) are larger; keys aligned to 16 bytes, room to read one
+// past an odd end.
+__device__ __forceinline__ int count_larger(const unsigned long long* keys, int n,
+                                            unsigned long long key) {
+  int rank = 0;
+#pragma unroll 4
+  for (int j = 0; j < n; j += 2) {
+    const ulonglong2 two = *reinterpret_cast<const ulonglong2*>(keys + j);
+    rank += two.x > key;
+    rank += j + 1 < n && two.y > key;
+  }
+  return rank;
+}
 
 // Keeps the k best of list[cur][0..kcur) and cand[0..n): each key's rank is
 // the number of larger ones. Ends with a barrier; returns how many are kept.
@@ -111,27 +159,34 @@ __device__ int merge(TopLds& L, int cur, int kcur, int n, int k) {
   const int all = kcur + n;
   for (int i = threadIdx.x; i < all; i += kWg) {
     const unsigned long long key = i < kcur ? L.list[cur][i] : L.cand[i - kcur];
-    int rank = 0;
-    for (int j = 0; j < kcur; ++j) rank += L.list[cur][j] > key;
-    for (int j = 0; j < n; ++j) rank += L.cand[j] > key;
+    const int rank = count_larger(L.list[cur], kcur, key) + count_larger(L.cand, n, key);
     if (rank < k) L.list[cur ^ 1][rank] = key;
   }
   __syncthreads();
   return all < k ? all : k;
 }
 
-// One workgroup per (row, share of the row's chunks).
+template <int TYPE>
+__device__ __forceinline__ float vec_max(const Vec<TYPE>& q) {
+  if constexpr (Vec<TYPE>::kVec == 8)
+    return max2(max3(q.get(0), q.get(1), q.get(2)),
+                max3(q.get(3), q.get(4), max3(q.get(5), q.get(6), q.get(7))));
+  else
+    return max2(max3(q.get(0), q.get(1), q.get(2)), q.get(3));
+}
+
+// One workgroup per (row, share of the row's units).
 template <int TYPE, bool TOP>
 __global__ __launch_bounds__(kWg) void k_logprobs(LogprobArgs a, int splits, int cps) {
   using El = Elem<TYPE>;
   using V = Vec<TYPE>;
-  constexpr int KV = V::kVec, U = kChunk / KV;
+  constexpr int KV = V::kVec, U = kVecs;
   __shared__ float fl[3][kWg / 64];
-  __shared__ int il[kWg / 64];
+  __shared__ int il[kWg / 64 + 1];
   __shared__ float row_ls;
   __shared__ TopLds L;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int V_ = static_cast<int>(a.V), nv = (V_ - 1) / KV + 1;
+  const int V_ = static_cast<int>(a.V), nv = V_ / KV, rest = V_ % KV;
   const float c = a.it * kLog2e, slack = kSlack / c;
   const int64_t work = a.T * splits;
   for (int64_t g = blockIdx.x; g < work; g += gridDim.x) {
@@ -144,57 +199,44 @@ __global__ __launch_bounds__(kWg) void k_logprobs(LogprobArgs a, int splits, int
     // what a logit must exceed to stand before the token: behind it and ahead
     const float gt = has ? xt : __builtin_huge_valf(), ge = has ? below(xt) : gt;
     const int tv = has ? static_cast<int>(tok) / KV : -1;  // the token's vector
-    const int v0 = min(nv, part * cps * (kWg * U)), v1 = min(nv, v0 + cps * (kWg * U));
+    const int v0 = min(nv, part * cps * (kUnit / KV)), v1 = min(nv, v0 + cps * (kUnit / KV));
 
-    float m = kNegInf, ref = kNegInf, rz = 0.0f, s = 0.0f, w = 0.0f;
+    float m = kNegInf, ref = kNegInf, rz = 0.0f, R = 0.0f, s = 0.0f, w = 0.0f;
     int ahead = 0, ahead_lane = 0;
+    bool bounded = false;                      // the row has met a masked logit (per wave)
     float th = kNegInf;
     int cur = 0, kcur = 0, pending = 0, parity = 0;
     int seen[2] = {0, 0};
     if (TOP && tid < 2) L.count[tid] = 0;
 
+    // what is left of the row past its whole vectors: an element to a lane
+    const bool owns_rest = part == splits - 1 && tid < rest;
+    const int jr = nv * KV + tid;
+    float lr = owns_rest ? El::load(x[jr]) : kNegInf;
     for (int vb = v0; vb < v1; vb += kWg * U) {
       V q[U];
-      float vm[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int v = vb + u * kWg + tid;
-        if (v < v1) {
-          const typename El::T* p = x + (int64_t)v * KV;
-          if (v < nv - 1 || V_ % KV == 0) q[u].load(p);
-          else q[u].load_part(p, V_ % KV);
-        } else {
-          q[u].fill_masked();
-        }
+        if (v < v1) q[u].load(x + (int64_t)v * KV);
+        else q[u].fill_masked();
       }
-      float cm = kNegInf;
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if constexpr (KV == 8)
-          vm[u] = max2(max3(q[u].get(0), q[u].get(1), q[u].get(2)),
-                       max3(q[u].get(3), q[u].get(4), max3(q[u].get(5), q[u].get(6), q[u].get(7))));
-        else
-          vm[u] = max2(max3(q[u].get(0), q[u].get(1), q[u].get(2)), q[u].get(3));
-        cm = max2(cm, vm[u]);
-      }
-      // (unpacked again below: kept, the 32 values would cost half the waves)
-#pragma unroll
-      for (int u = 0; u < U; ++u) asm("" : "+v"(q[u].q[0]), "+v"(q[u].q[1]), "+v"(q[u].q[2]), "+v"(q[u].q[3]));
-      if (cm > ref + slack) {
-        move_to(cm, ref, c, s, w);
-        ref = rz = cm;
-      }
-      m = max2(m, cm);
       if (TOP && vb == v0) {
         // the wave's k-th largest lane maximum; its low bits give way to the
         // lane, which only lowers it
-        const unsigned u = __float_as_uint((cm == cm ? cm : kNegInf) + 0.0f);
-        const unsigned key = (((u & 0x80000000u) ? ~u : (u | 0x80000000u)) & ~63u) | (63 - lane);
+        float cm = kNegInf;
+#pragma unroll
+        for (int u = 0; u < U; ++u) cm = max2(cm, vec_max<TYPE>(q[u]));
+        const unsigned key = (code_of(cm == cm ? cm : kNegInf) & ~63u) | (63 - lane);
         L.lane_max[tid] = key;
         __syncthreads();
         int rank = 0;
-#pragma unroll 16
-        for (int j = 0; j < 64; ++j) rank += L.lane_max[(tid & ~63) + j] > key;
+        const uint4* four = reinterpret_cast<const uint4*>(L.lane_max + (tid & ~63));
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const uint4 o = four[j];
+          rank += (o.x > key) + (o.y > key) + (o.z > key) + (o.w > key);
+        }
         const unsigned long long who = __ballot(rank == a.top - 1);
         const unsigned kth = __builtin_amdgcn_readlane(key, __builtin_ctzll(who)) & ~63u;
         if (lane == 0) L.wave_th[wave] = ordered_value(kth);
@@ -205,30 +247,66 @@ __global__ __launch_bounds__(kWg) void k_logprobs(LogprobArgs a, int splits, int
           if (L.wave_th[i] > th) th = L.wave_th[i];
         if (th > kNegInf) th = below(th);
       }
+      const auto pass = [&](auto is_bounded, auto is_first) {
+        constexpr bool BOUNDED = decltype(is_bounded)::value, FIRST = decltype(is_first)::value;
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (vb + u * kWg + wave * 64 >= v1) break;
-        const int v = vb + u * kWg + tid;
-        const float thr = v < tv ? ge : gt;
-        if (v == tv) {                                     // one lane of one chunk
-          for (int64_t j = (int64_t)v * KV; j < tok; ++j) ahead_lane += El::load(x[j]) == xt;
-        }
-#pragma unroll
-        for (int e = 0; e < KV; ++e) {
-          const float l = q[u].get(e), t = (l - rz) * c, ex = __builtin_amdgcn_exp2f(t);
-          s += ex;
-          w = fmaf(ex, max2(t, kLow), w);
-          ahead += __builtin_popcountll(__ballot(l > thr));
-        }
-        if (TOP && !(vm[u] <= th)) {
+        for (int u = 0; u < U; ++u) {
+          if (vb + u * kWg + wave * 64 >= v1) break;
+          const float vm = vec_max<TYPE>(q[u]);
+          if (vm > ref + slack) {
+            move_to(vm, ref, c, s, w);
+            ref = rz = vm;
+            R = scaled_ref(vm, c);
+          }
+          const int v = vb + u * kWg + tid;
+          const float thr = v < tv ? ge : gt;
+          const float off = BOUNDED && fabsf(rz) < kFar ? fmaf(rz, c, -R) : 0.0f;
 #pragma unroll
           for (int e = 0; e < KV; ++e) {
             const float l = q[u].get(e);
-            if (l > th) {
-              const int at = pending + atomicAdd(&L.count[parity], 1) - seen[parity];
-              if (at < kCand) L.cand[at] = pack_key(l, static_cast<unsigned>(v) * KV + e);
+            const float t = BOUNDED ? fmaf(l - rz, c, off) : fmaf(l, c, -R);
+            const float ex = __builtin_amdgcn_exp2f(t);
+            s += ex;
+            w = fmaf(ex, BOUNDED ? max2(t, kLow) : t, w);
+            if (FIRST) ahead += __builtin_popcountll(__ballot(l > thr));
+          }
+          if (!FIRST) continue;
+          m = max2(m, vm);
+          if (v == tv) {                                   // one lane of one chunk
+            for (int64_t j = (int64_t)v * KV; j < tok; ++j) ahead_lane += El::load(x[j]) == xt;
+          }
+          if (TOP && !(vm <= th)) {
+            V left = q[u];
+#pragma unroll 1
+            for (int i = 0; i < 4; ++i) {
+#pragma unroll
+              for (int e = 0; e < KV / 4; ++e) {
+                const float l = left.get(e);
+                if (l > th) {
+                  const int at = pending + atomicAdd(&L.count[parity], 1) - seen[parity];
+                  if (at < kCand) L.cand[at] = pack_key(l, static_cast<unsigned>(v) * KV + i * (KV / 4) + e);
+                }
+              }
+              left.q[0] = left.q[1];
+              left.q[1] = left.q[2];
+              left.q[2] = left.q[3];
             }
           }
+        }
+      };
+      if (bounded) {
+        pass(std::true_type(), std::true_type());
+      } else {
+        const float s0 = s, w0 = w, ref0 = ref, rz0 = rz, R0 = R;
+        pass(std::false_type(), std::true_type());
+        if (__any(!(fabsf(w) < __builtin_huge_valf()))) {
+          bounded = true;
+          s = s0;
+          w = w0;
+          ref = ref0;
+          rz = rz0;
+          R = R0;
+          pass(std::true_type(), std::false_type());
         }
       }
       if (TOP) {
@@ -241,7 +319,7 @@ __global__ __launch_bounds__(kWg) void k_logprobs(LogprobArgs a, int splits, int
           // the chunk again, 256 candidates at a time
           kcur = merge(L, cur, kcur, pending, a.top);
           cur ^= 1;
-          const int64_t j0 = (int64_t)vb * KV, j1 = min(a.V, j0 + kWg * kChunk);
+          const int64_t j0 = (int64_t)vb * KV, j1 = min(a.V, j0 + kWg * U * KV);
           for (int64_t j = j0; j < j1; j += kWg) {
             const unsigned long long least = kcur == a.top ? L.list[cur][kcur - 1] : 0ull;
             if (j + tid < j1) {
@@ -264,11 +342,9 @@ __global__ __launch_bounds__(kWg) void k_logprobs(LogprobArgs a, int splits, int
           th = kcur == a.top ? key_value(L.list[cur][kcur - 1]) : kNegInf;
         } else {
           pending += got;
-          if (pending >= kMergeAt || vb + kWg * U >= v1) {
-            if (pending > 0) {
-              kcur = merge(L, cur, kcur, pending, a.top);
-              cur ^= 1;
-            }
+          if (pending >= kMergeAt) {
+            kcur = merge(L, cur, kcur, pending, a.top);
+            cur ^= 1;
             pending = 0;
             th = kcur == a.top ? key_value(L.list[cur][kcur - 1]) : kNegInf;
           }
@@ -276,24 +352,51 @@ __global__ __launch_bounds__(kWg) void k_logprobs(LogprobArgs a, int splits, int
       }
     }
 
+    if (rest > 0 && part == splits - 1 && wave == 0) {
+      if (lr > ref + slack) {
+        move_to(lr, ref, c, s, w);
+        ref = rz = lr;
+        R = scaled_ref(lr, c);
+      }
+      m = max2(m, lr);
+      const float t = fmaf(lr - rz, c, fabsf(rz) < kFar ? fmaf(rz, c, -R) : 0.0f);
+      const float ex = __builtin_amdgcn_exp2f(t);
+      s += ex;
+      w = fmaf(ex, max2(t, kLow), w);
+      ahead += __builtin_popcountll(__ballot(lr > (jr < tok ? ge : gt)));
+    }
+    if (TOP) {
+      __syncthreads();                         // (a row without whole vectors: the counters)
+      if (lr > th) {
+        const int at = pending + atomicAdd(&L.count[parity], 1) - seen[parity];
+        L.cand[at] = pack_key(lr, static_cast<unsigned>(jr));
+      }
+      __syncthreads();
+      pending += L.count[parity] - seen[parity];
+      if (pending > 0) {
+        kcur = merge(L, cur, kcur, pending, a.top);
+        cur ^= 1;
+      }
+    }
+
     // join the lanes
     float M = wave_max(m);
     if (lane == 0) fl[0][wave] = M;
+    if (tid == 0) il[kWg / 64] = 0;
     __syncthreads();
     for (int i = 0; i < kWg / 64; ++i) M = fmaxf(M, fl[0][i]);
     move_to(M, ref, c, s, w);
     s = wave_sum(s);
     w = wave_sum(w);
-    int al = ahead_lane;
-    for (int off = 32; off > 0; off >>= 1) al += __shfl_xor(al, off);
+    if (ahead_lane) il[kWg / 64] = ahead_lane;       // (the token's lane, or none)
     if (lane == 0) {
       fl[1][wave] = s;
       fl[2][wave] = w;
-      il[wave] = ahead + al;
+      il[wave] = ahead;
     }
     __syncthreads();
     if (tid == 0) {
-      Partial p{M, fl[1][0], fl[2][0], il[0]};
+      Partial p{M, fl[1][0], fl[2][0], il[0] + il[kWg / 64]};
       for (int i = 1; i < kWg / 64; ++i) {
         p.s += fl[1][i];
         p.w += fl[2][i];
@@ -323,7 +426,8 @@ constexpr int kMaxJoinKeys = 1024;
 template <int TYPE>
 __global__ __launch_bounds__(kWg) void k_logprobs_join(LogprobArgs a, int splits) {
   using El = Elem<TYPE>;
-  __shared__ unsigned long long keys[kMaxJoinKeys];
+  __shared__ alignas(16) unsigned long long keys[kMaxJoinKeys + 2];
+  __shared__ int count;
   __shared__ unsigned long long best[BO_MAX_ALTERNATIVES];
   __shared__ float row_M, row_ls;
   const int tid = threadIdx.x;
@@ -333,9 +437,12 @@ __global__ __launch_bounds__(kWg) void k_logprobs_join(LogprobArgs a, int splits
     const unsigned long long* ks =
         reinterpret_cast<const unsigned long long*>(static_cast<const Partial*>(a.ws) + a.T * splits) +
         row * splits * a.top;
-    const int n = splits * a.top;
-    for (int i = tid; i < n; i += kWg) keys[i] = ks[i];
+    // a bound that `top` keys reach: every share's p-th best
+    const int n = splits * a.top, p = (a.top + splits - 1) / splits;
     for (int i = tid; i < a.top; i += kWg) best[i] = 0ull;
+    if (tid == 0) count = 0;
+    unsigned long long bound = ~0ull;
+    for (int i = 0; i < splits && a.top > 0; ++i) bound = min(bound, ks[i * a.top + p - 1]);
     if (tid < 64) {
       Partial p{kNegInf, 0.0f, 0.0f, 0};
       if (tid < splits) p = ps[tid];
@@ -355,10 +462,13 @@ __global__ __launch_bounds__(kWg) void k_logprobs_join(LogprobArgs a, int splits
     }
     __syncthreads();
     for (int i = tid; i < n; i += kWg) {
-      const unsigned long long key = keys[i];
-      int rank = 0;
-      for (int j = 0; j < n; ++j) rank += keys[j] > key;
-      if (key && rank < a.top) best[rank] = key;
+      const unsigned long long key = ks[i];
+      if (key && key >= bound) keys[atomicAdd(&count, 1)] = key;
+    }
+    __syncthreads();
+    for (int i = tid; i < count; i += kWg) {
+      const int rank = count_larger(keys, count, keys[i]);
+      if (rank < a.top) best[rank] = keys[i];
     }
     __syncthreads();
     if (tid < a.top) finish_top(a, row, tid, best[tid], row_M, row_ls);
@@ -374,11 +484,11 @@ template <int TYPE>
 __global__ __launch_bounds__(kWg) void k_logprobs_grad(LogprobGradArgs a, int splits, int cps) {
   using El = Elem<TYPE>;
   using V = Vec<TYPE>;
-  constexpr int KV = V::kVec, U = kChunk / KV;
+  constexpr int KV = V::kVec, U = kVecs;
   __shared__ float hot[BO_MAX_ALTERNATIVES + 1];
   __shared__ int at[BO_MAX_ALTERNATIVES + 1];
   const int tid = threadIdx.x;
-  const int V_ = static_cast<int>(a.V), nv = (V_ - 1) / KV + 1;
+  const int V_ = static_cast<int>(a.V), nv = V_ / KV, rest = V_ % KV;
   const float c = a.it * kLog2e;
   const int64_t work = a.T * splits;
   for (int64_t g = blockIdx.x; g < work; g += gridDim.x) {
@@ -386,7 +496,7 @@ __global__ __launch_bounds__(kWg) void k_logprobs_grad(LogprobGradArgs a, int sp
     const int part = splits == 1 ? 0 : static_cast<int>(g - row * splits);
     const typename El::T* x = static_cast<const typename El::T*>(a.logits) + row * a.stride;
     typename El::T* out = static_cast<typename El::T*>(a.out) + row * a.out_stride;
-    const int v0 = min(nv, part * cps * (kWg * U)), v1 = min(nv, v0 + cps * (kWg * U));
+    const int v0 = min(nv, part * cps * (kUnit / KV)), v1 = min(nv, v0 + cps * (kUnit / KV));
     const float m0 = a.stats[2 * row], ls0 = a.stats[2 * row + 1];
     const bool empty = m0 == kNegInf && ls0 == kNegInf;
     const float m = empty ? 0.0f : m0, ls2 = empty ? 0.0f : ls0 * kLog2e;
@@ -409,7 +519,11 @@ __global__ __launch_bounds__(kWg) void k_logprobs_grad(LogprobGradArgs a, int sp
       at[tid] = id;
       hot[tid] = own;
     }
-    if (id < v0 * (int64_t)KV || id >= v1 * (int64_t)KV || empty) id = -1;
+    // (the row's last share has what is left past the whole vectors)
+    const bool last = part == splits - 1;
+    if (id < v0 * KV || id >= (last ? V_ : v1 * KV) || empty) id = -1;
+    const int jr = nv * KV + tid;
+    const float lr = last && tid < rest ? El::load(x[jr]) : 0.0f;
     const float xi = id >= 0 ? El::load(x[id]) : 0.0f;     // before the row may be overwritten
     __syncthreads();
     float total = 0.0f, mine = 0.0f;
@@ -429,11 +543,7 @@ __global__ __launch_bounds__(kWg) void k_logprobs_grad(LogprobGradArgs a, int sp
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int v = vb + u * kWg + tid;
-        if (v < v1) {
-          const typename El::T* p = x + (int64_t)v * KV;
-          if (v < nv - 1 || V_ % KV == 0) q[u].load(p);
-          else q[u].load_part(p, V_ % KV);
-        }
+        if (v < v1) q[u].load(x + (int64_t)v * KV);
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
@@ -443,12 +553,11 @@ __global__ __launch_bounds__(kWg) void k_logprobs_grad(LogprobGradArgs a, int sp
 #pragma unroll
           for (int e = 0; e < KV; ++e) r[e] = grad(q[u].get(e));
           q[u].set_all(r);
-          typename El::T* p = out + (int64_t)v * KV;
-          if (v < nv - 1 || V_ % KV == 0) q[u].store(p);
-          else q[u].store_part(p, V_ % KV);
+          q[u].store(out + (int64_t)v * KV);
         }
       }
     }
+    if (last && tid < rest) out[jr] = El::store(grad(lr));
     __syncthreads();
     // (an id that is given twice has all its terms in each of its threads)
     if (id >= 0) out[id] = El::store(grad(xi) + a.it * mine);
@@ -457,12 +566,12 @@ __global__ __launch_bounds__(kWg) void k_logprobs_grad(LogprobGradArgs a, int sp
 }
 
 // Shares of a row: enough workgroups for every compute unit when the rows are
-// few, whole chunks each.
+// few, whole units each.
 struct Split {
   int splits, cps;
 };
 Split split_of(int64_t T, int64_t V, int top) {
-  const int64_t chunks = (V + kWg * kChunk - 1) / (kWg * kChunk);
+  const int64_t chunks = (V + kUnit - 1) / kUnit;
   int64_t want = T >= 1024 ? 1 : 1024 / T;
   want = std::min<int64_t>({want, chunks, kMaxSplits, top > 0 ? kMaxJoinKeys / top : kMaxSplits});
   const int64_t cps = (chunks + want - 1) / want;

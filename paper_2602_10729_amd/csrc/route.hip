@@ -84,12 +84,8 @@ __device__ __forceinline__ void keep_best(double* a, const double* b) {
   bitonic<K>(a);
 }
 
-// The value's order-preserving code (-0 as +0), and its key with the place
-// among the lane's experts. v is no NaN; -inf is none.
-__device__ __forceinline__ unsigned code_of(float v) {
-  const unsigned u = __float_as_uint(v + 0.0f);
-  return u ^ (static_cast<unsigned>(static_cast<int>(u) >> 31) | 0x80000000u);
-}
+// The value's key with the place among the lane's experts. v is no NaN; -inf is
+// none.
 __device__ __forceinline__ double make_key(float v, int place) {
   const unsigned o = code_of(v);
   return __hiloint2double(static_cast<int>(kExpTwo52 | (o >> 12)),

@@ -42,13 +42,16 @@ struct Vec {
   // system takes a 16-byte access at every address.
   __device__ __forceinline__ void load(const T* p) { __builtin_memcpy(q, p, 16); }
   __device__ __forceinline__ void store(T* p) const { __builtin_memcpy(p, q, 16); }
-  // the first n >= 1 elements, the rest -inf (the first one read again)
+  // the first n elements, the rest -inf (the first one read again)
   __device__ __forceinline__ void load_part(const T* p, int n) {
-    const uint32_t none = bits_of(Elem<TYPE>::store(-__builtin_huge_valf()));
+    fill_masked();
 #pragma unroll
     for (int e = 0; e < kVec; ++e) {
       const uint32_t b = bits_of(p[e < n ? e : 0]);
-      set_bits(e, e < n ? b : none);
+      if (e < n) {
+        if constexpr (kVec == 4) q[e] = b;
+        else q[e / 2] = (e & 1) ? (q[e / 2] & 0xFFFFu) | (b << 16) : (q[e / 2] & 0xFFFF0000u) | b;
+      }
     }
   }
   __device__ __forceinline__ void store_part(T* p, int n) const {
@@ -101,18 +104,17 @@ struct Vec {
       return h;
     }
   }
-  __device__ __forceinline__ void set_bits(int e, uint32_t b) {
-    if constexpr (kVec == 4) q[e] = b;
-    else q[e / 2] = (e & 1) ? (q[e / 2] & 0xFFFFu) | (b << 16) : (q[e / 2] & 0xFFFF0000u) | b;
-  }
 };
 
-// Larger value first, the lower index among equals, as the unsigned order of
-// one 64-bit key (-0 and +0 are equal); 0 is below every key of a value.
-__device__ __forceinline__ unsigned long long pack_key(float v, unsigned j) {
+// A value's order as an unsigned number (-0 and +0 are equal).
+__device__ __forceinline__ unsigned code_of(float v) {
   const unsigned u = __float_as_uint(v + 0.0f);
-  const unsigned o = (u & 0x80000000u) ? ~u : (u | 0x80000000u);
-  return (static_cast<unsigned long long>(o) << 32) | (0xFFFFFFFFu - j);
+  return u ^ (static_cast<unsigned>(static_cast<int>(u) >> 31) | 0x80000000u);
+}
+// Larger value first, the lower index among equals, as the unsigned order of
+// one 64-bit key; 0 is below every key of a value.
+__device__ __forceinline__ unsigned long long pack_key(float v, unsigned j) {
+  return (static_cast<unsigned long long>(code_of(v)) << 32) | (0xFFFFFFFFu - j);
 }
 __device__ __forceinline__ float ordered_value(unsigned o) {
   return __uint_as_float((o & 0x80000000u) ? (o & 0x7FFFFFFFu) : ~o);
