@@ -215,11 +215,14 @@ __global__ __launch_bounds__(kWg) void k_logprobs(LogprobArgs a, int splits, int
     float lr = owns_rest ? El::load(x[jr]) : kNegInf;
     for (int vb = v0; vb < v1; vb += kWg * U) {
       V q[U];
+      // (every lane loads, past the share its last vector again: a load that only
+      // some lanes make waits for the one before)
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int v = vb + u * kWg + tid;
-        if (v < v1) q[u].load(x + (int64_t)v * KV);
-        else q[u].fill_masked();
+      for (int u = 0; u < U; ++u) q[u].load(x + (int64_t)min(vb + u * kWg + tid, v1 - 1) * KV);
+      if (vb + kWg * U > v1) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (vb + u * kWg + tid >= v1) q[u].fill_masked();
       }
       if (TOP && vb == v0) {
         // the wave's k-th largest lane maximum; its low bits give way to the
@@ -541,10 +544,7 @@ __global__ __launch_bounds__(kWg) void k_logprobs_grad(LogprobGradArgs a, int sp
     for (int vb = v0; vb < v1; vb += kWg * U) {
       V q[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int v = vb + u * kWg + tid;
-        if (v < v1) q[u].load(x + (int64_t)v * KV);
-      }
+      for (int u = 0; u < U; ++u) q[u].load(x + (int64_t)min(vb + u * kWg + tid, v1 - 1) * KV);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int v = vb + u * kWg + tid;
