@@ -201,7 +201,14 @@ __global__ __launch_bounds__(kWg) void k_logprobs(LogprobArgs a, int splits, int
     const int tv = has ? static_cast<int>(tok) / KV : -1;  // the token's vector
     const int v0 = min(nv, part * cps * (kUnit / KV)), v1 = min(nv, v0 + cps * (kUnit / KV));
 
-    float m = kNegInf, ref = kNegInf, rz = 0.0f, R = 0.0f, s = 0.0f, w = 0.0f;
+    // the lane's reference: itself, as it is subtracted (0 for none), scaled, and
+    // what a logit must exceed to move it
+    float m = kNegInf, ref = kNegInf, rz = 0.0f, R = 0.0f, lim = kNegInf, s = 0.0f, w = 0.0f;
+    const auto set_ref = [&](float r) {
+      ref = rz = r;
+      R = scaled_ref(r, c);
+      lim = r + slack;
+    };
     int ahead = 0, ahead_lane = 0;
     bool bounded = false;                      // the row has met a masked logit (per wave)
     float th = kNegInf;
@@ -215,10 +222,12 @@ __global__ __launch_bounds__(kWg) void k_logprobs(LogprobArgs a, int splits, int
     float lr = owns_rest ? El::load(x[jr]) : kNegInf;
     for (int vb = v0; vb < v1; vb += kWg * U) {
       V q[U];
+      const typename El::T* xc = x + (int64_t)vb * KV;
       // (every lane loads, past the share its last vector again: a load that only
       // some lanes make waits for the one before)
 #pragma unroll
-      for (int u = 0; u < U; ++u) q[u].load(x + (int64_t)min(vb + u * kWg + tid, v1 - 1) * KV);
+      for (int u = 0; u < U; ++u)
+        q[u].load(xc + static_cast<unsigned>(min(u * kWg + tid, v1 - 1 - vb)) * KV);
       if (vb + kWg * U > v1) {
 #pragma unroll
         for (int u = 0; u < U; ++u)
@@ -256,14 +265,18 @@ __global__ __launch_bounds__(kWg) void k_logprobs(LogprobArgs a, int splits, int
         for (int u = 0; u < U; ++u) {
           if (vb + u * kWg + wave * 64 >= v1) break;
           const float vm = vec_max<TYPE>(q[u]);
-          if (vm > ref + slack) {
+          if (vm > lim) {
             move_to(vm, ref, c, s, w);
-            ref = rz = vm;
-            R = scaled_ref(vm, c);
+            set_ref(vm);
           }
           const int v = vb + u * kWg + tid;
           const float thr = v < tv ? ge : gt;
           const float off = BOUNDED && fabsf(rz) < kFar ? fmaf(rz, c, -R) : 0.0f;
+          // (a token among its row's likeliest: few vectors hold what precedes it)
+          if (FIRST && __any(vm > thr)) {
+#pragma unroll
+            for (int e = 0; e < KV; ++e) ahead += __builtin_popcountll(__ballot(q[u].get(e) > thr));
+          }
 #pragma unroll
           for (int e = 0; e < KV; ++e) {
             const float l = q[u].get(e);
@@ -271,7 +284,6 @@ __global__ __launch_bounds__(kWg) void k_logprobs(LogprobArgs a, int splits, int
             const float ex = __builtin_amdgcn_exp2f(t);
             s += ex;
             w = fmaf(ex, BOUNDED ? max2(t, kLow) : t, w);
-            if (FIRST) ahead += __builtin_popcountll(__ballot(l > thr));
           }
           if (!FIRST) continue;
           m = max2(m, vm);
@@ -300,15 +312,18 @@ __global__ __launch_bounds__(kWg) void k_logprobs(LogprobArgs a, int splits, int
       if (bounded) {
         pass(std::true_type(), std::true_type());
       } else {
-        const float s0 = s, w0 = w, ref0 = ref, rz0 = rz, R0 = R;
+        const float s0 = s, w0 = w, ref0 = ref;
         pass(std::false_type(), std::true_type());
         if (__any(!(fabsf(w) < __builtin_huge_valf()))) {
           bounded = true;
           s = s0;
           w = w0;
-          ref = ref0;
-          rz = rz0;
-          R = R0;
+          if (ref0 > kNegInf) {
+            set_ref(ref0);
+          } else {
+            ref = lim = kNegInf;
+            rz = R = 0.0f;
+          }
           pass(std::true_type(), std::false_type());
         }
       }
@@ -356,10 +371,9 @@ __global__ __launch_bounds__(kWg) void k_logprobs(LogprobArgs a, int splits, int
     }
 
     if (rest > 0 && part == splits - 1 && wave == 0) {
-      if (lr > ref + slack) {
+      if (lr > lim) {
         move_to(lr, ref, c, s, w);
-        ref = rz = lr;
-        R = scaled_ref(lr, c);
+        set_ref(lr);
       }
       m = max2(m, lr);
       const float t = fmaf(lr - rz, c, fabsf(rz) < kFar ? fmaf(rz, c, -R) : 0.0f);
