@@ -102,6 +102,14 @@ __device__ __forceinline__ void move_to(float M, float r, float c, float& s, flo
   if (M - M != 0.0f) s = w = __builtin_nanf("");
 }
 
+// Workgroups go to the chip's dies in turn. Rows in that order would give all
+// rows of a batch that are alike by a period of 2, 4 or 8 (masked ones cost more)
+// to the same dies; a die takes consecutive rows instead.
+constexpr int kXcds = 8;
+__device__ __forceinline__ int64_t xcd_order(int64_t b, int64_t each) {
+  return (b % kXcds) * each + b / kXcds;
+}
+
 struct Partial {      // of one row's share
   float M, s, w;
   int ahead;
@@ -111,7 +119,7 @@ struct Partial {      // of one row's share
 __device__ __forceinline__ float finish(const LogprobArgs& a, int64_t row, const Partial& p,
                                         int64_t tok, float xt) {
   const bool has = tok >= 0 && tok < a.V;
-  const float c = a.it * kLog2e;
+  const float c = a.c;
   const float lost = fabsf(p.M) < kFar ? fmaf(p.M, c, -scaled_ref(p.M, c)) : 0.0f;
   const float ls0 = logf(p.s), ls = ls0 - lost * kLn2;
   a.stats[2 * row] = p.M;
@@ -187,9 +195,11 @@ __global__ __launch_bounds__(kWg) void k_logprobs(LogprobArgs a, int splits, int
   __shared__ TopLds L;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int V_ = static_cast<int>(a.V), nv = V_ / KV, rest = V_ % KV;
-  const float c = a.it * kLog2e, slack = kSlack / c;
-  const int64_t work = a.T * splits;
-  for (int64_t g = blockIdx.x; g < work; g += gridDim.x) {
+  const float c = a.c, slack = a.slack;
+  const int64_t work = a.T * splits, each = (work + kXcds - 1) / kXcds;
+  for (int64_t b = blockIdx.x; b < each * kXcds; b += gridDim.x) {
+    const int64_t g = xcd_order(b, each);
+    if (g >= work) continue;
     const int64_t row = splits == 1 ? g : g / splits;
     const int part = splits == 1 ? 0 : static_cast<int>(g - row * splits);
     const typename El::T* x = static_cast<const typename El::T*>(a.logits) + row * a.stride;
@@ -448,7 +458,7 @@ __global__ __launch_bounds__(kWg) void k_logprobs_join(LogprobArgs a, int splits
   __shared__ unsigned long long best[BO_MAX_ALTERNATIVES];
   __shared__ float row_M, row_ls;
   const int tid = threadIdx.x;
-  const float c = a.it * kLog2e;
+  const float c = a.c;
   for (int64_t row = blockIdx.x; row < a.T; row += gridDim.x) {
     const Partial* ps = static_cast<const Partial*>(a.ws) + row * splits;
     const unsigned long long* ks =
@@ -595,7 +605,7 @@ Split split_of(int64_t T, int64_t V, int top) {
 template <int TYPE>
 hipError_t launch(const LogprobArgs& a, hipStream_t st) {
   const Split sp = split_of(a.T, a.V, a.top);
-  const int64_t work = a.T * sp.splits;
+  const int64_t work = (a.T * sp.splits + kXcds - 1) / kXcds * kXcds;
   const dim3 grid(static_cast<unsigned>(std::min<int64_t>(work, 1 << 22)));
   if (a.top > 0) k_logprobs<TYPE, true><<<grid, kWg, 0, st>>>(a, sp.splits, sp.cps);
   else k_logprobs<TYPE, false><<<grid, kWg, 0, st>>>(a, sp.splits, sp.cps);
@@ -612,7 +622,10 @@ int64_t logprob_workspace(int64_t T, int64_t V, int top) {
   return sp.splits == 1 ? 0 : T * sp.splits * static_cast<int64_t>(sizeof(Partial) + 8 * top);
 }
 
-hipError_t launch_logprobs(const LogprobArgs& a, hipStream_t st) {
+hipError_t launch_logprobs(const LogprobArgs& args, hipStream_t st) {
+  LogprobArgs a = args;
+  a.c = a.it * kLog2e;
+  a.slack = kSlack / a.c;
   if (a.type == BO_TYPE_F32) return launch<BO_TYPE_F32>(a, st);
   if (a.type == BO_TYPE_BF16) return launch<BO_TYPE_BF16>(a, st);
   return launch<BO_TYPE_F16>(a, st);

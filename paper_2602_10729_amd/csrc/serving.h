@@ -134,6 +134,7 @@ struct LogprobArgs {
   int64_t T, V, stride;
   const int64_t* tokens;       // or nullptr
   float it;                    // inverse temperature
+  float c, slack;              // log2(e) it; how far a reference may lag, in logits
   int top;
   float* logprob;
   int32_t* rank;

@@ -136,7 +136,7 @@ bo_status bo_token_logprobs(const void* logits, int32_t type, int64_t T, int64_t
     }
     if ((s = check_workspace(workspace, workspace_bytes, bo::logprob_workspace(T, V, top), W)) != BO_OK)
       return s;
-    bo::LogprobArgs a{logits, type, T, V, stride, tokens, inv_temperature, top, logprob, rank,
+    bo::LogprobArgs a{logits, type, T, V, stride, tokens, inv_temperature, 0.0f, 0.0f, top, logprob, rank,
                       entropy, stats, top_ids, top_logprobs, workspace};
     hipStream_t st = static_cast<hipStream_t>(stream);
     return bo::after_launch(bo::launch_logprobs(a, st), st, W);
