@@ -203,13 +203,23 @@ __global__ __launch_bounds__(kWg) void k_logprobs(LogprobArgs a, int splits, int
     const int64_t row = splits == 1 ? g : g / splits;
     const int part = splits == 1 ? 0 : static_cast<int>(g - row * splits);
     const typename El::T* x = static_cast<const typename El::T*>(a.logits) + row * a.stride;
+    const int v0 = min(nv, part * cps * (kUnit / KV)), v1 = min(nv, v0 + cps * (kUnit / KV));
+    // a chunk: every lane loads, past the share its last vector again (a load
+    // that only some lanes make waits for the one before)
+    V q[U];
+    const auto fetch = [&](int vb) {
+      const typename El::T* xc = x + (int64_t)vb * KV;
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        q[u].load(xc + static_cast<unsigned>(min(u * kWg + tid, v1 - 1 - vb)) * KV);
+    };
+    if (v0 < v1) fetch(v0);
     const int64_t tok = a.tokens ? a.tokens[row] : -1;
     const bool has = tok >= 0 && tok < a.V;
     const float xt = has ? El::load(x[tok]) : 0.0f;
     // what a logit must exceed to stand before the token: behind it and ahead
     const float gt = has ? xt : __builtin_huge_valf(), ge = has ? below(xt) : gt;
     const int tv = has ? static_cast<int>(tok) / KV : -1;  // the token's vector
-    const int v0 = min(nv, part * cps * (kUnit / KV)), v1 = min(nv, v0 + cps * (kUnit / KV));
 
     // the lane's reference: itself, as it is subtracted (0 for none), scaled, and
     // what a logit must exceed to move it
@@ -231,13 +241,6 @@ __global__ __launch_bounds__(kWg) void k_logprobs(LogprobArgs a, int splits, int
     const int jr = nv * KV + tid;
     float lr = owns_rest ? El::load(x[jr]) : kNegInf;
     for (int vb = v0; vb < v1; vb += kWg * U) {
-      V q[U];
-      const typename El::T* xc = x + (int64_t)vb * KV;
-      // (every lane loads, past the share its last vector again: a load that only
-      // some lanes make waits for the one before)
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        q[u].load(xc + static_cast<unsigned>(min(u * kWg + tid, v1 - 1 - vb)) * KV);
       if (vb + kWg * U > v1) {
 #pragma unroll
         for (int u = 0; u < U; ++u)
@@ -300,21 +303,14 @@ __global__ __launch_bounds__(kWg) void k_logprobs(LogprobArgs a, int splits, int
           if (v == tv) {                                   // one lane of one chunk
             for (int64_t j = (int64_t)v * KV; j < tok; ++j) ahead_lane += El::load(x[j]) == xt;
           }
-          if (TOP && !(vm <= th)) {
-            V left = q[u];
-#pragma unroll 1
-            for (int i = 0; i < 4; ++i) {
+          if (TOP && __any(!(vm <= th))) {
 #pragma unroll
-              for (int e = 0; e < KV / 4; ++e) {
-                const float l = left.get(e);
-                if (l > th) {
-                  const int at = pending + atomicAdd(&L.count[parity], 1) - seen[parity];
-                  if (at < kCand) L.cand[at] = pack_key(l, static_cast<unsigned>(v) * KV + i * (KV / 4) + e);
-                }
+            for (int e = 0; e < KV; ++e) {
+              const float l = q[u].get(e);
+              if (__any(l > th) && l > th) {
+                const int at = pending + atomicAdd(&L.count[parity], 1) - seen[parity];
+                if (at < kCand) L.cand[at] = pack_key(l, static_cast<unsigned>(v) * KV + e);
               }
-              left.q[0] = left.q[1];
-              left.q[1] = left.q[2];
-              left.q[2] = left.q[3];
             }
           }
         }
@@ -337,6 +333,7 @@ __global__ __launch_bounds__(kWg) void k_logprobs(LogprobArgs a, int splits, int
           pass(std::true_type(), std::false_type());
         }
       }
+      if (vb + kWg * U < v1) fetch(vb + kWg * U);     // (on its way during the barrier)
       if (TOP) {
         __syncthreads();
         const int got = L.count[parity] - seen[parity];
@@ -370,7 +367,7 @@ __global__ __launch_bounds__(kWg) void k_logprobs(LogprobArgs a, int splits, int
           th = kcur == a.top ? key_value(L.list[cur][kcur - 1]) : kNegInf;
         } else {
           pending += got;
-          if (pending >= kMergeAt) {
+          if (pending >= kMergeAt || (vb == v0 && pending > a.top)) {
             kcur = merge(L, cur, kcur, pending, a.top);
             cur ^= 1;
             pending = 0;
@@ -468,8 +465,12 @@ __global__ __launch_bounds__(kWg) void k_logprobs_join(LogprobArgs a, int splits
     const int n = splits * a.top, p = (a.top + splits - 1) / splits;
     for (int i = tid; i < a.top; i += kWg) best[i] = 0ull;
     if (tid == 0) count = 0;
-    unsigned long long bound = ~0ull;
-    for (int i = 0; i < splits && a.top > 0; ++i) bound = min(bound, ks[i * a.top + p - 1]);
+    unsigned long long key[kMaxJoinKeys / kWg];
+#pragma unroll
+    for (int i = 0; i < kMaxJoinKeys / kWg; ++i) key[i] = i * kWg + tid < n ? ks[i * kWg + tid] : 0ull;
+    const int lane = tid & 63;
+    unsigned long long bound = a.top > 0 && lane < splits ? ks[lane * a.top + p - 1] : ~0ull;
+    for (int off = 32; off > 0; off >>= 1) bound = min(bound, __shfl_xor(bound, off));
     if (tid < 64) {
       Partial p{kNegInf, 0.0f, 0.0f, 0};
       if (tid < splits) p = ps[tid];
@@ -488,10 +489,9 @@ __global__ __launch_bounds__(kWg) void k_logprobs_join(LogprobArgs a, int splits
       }
     }
     __syncthreads();
-    for (int i = tid; i < n; i += kWg) {
-      const unsigned long long key = ks[i];
-      if (key && key >= bound) keys[atomicAdd(&count, 1)] = key;
-    }
+#pragma unroll
+    for (int i = 0; i < kMaxJoinKeys / kWg; ++i)
+      if (key[i] && key[i] >= bound) keys[atomicAdd(&count, 1)] = key[i];
     __syncthreads();
     for (int i = tid; i < count; i += kWg) {
       const int rank = count_larger(keys, count, keys[i]);
