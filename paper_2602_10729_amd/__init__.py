@@ -146,6 +146,23 @@ def _stream(stream):
     return ctypes.c_void_p(int(stream.cuda_stream))
 
 
+_raw_stream = None
+
+
+def _stream_of(t, stream):
+    """The stream's handle for a call on tensor t: torch's current stream of its
+    device, read without building a stream object (0.1 us instead of 3) where
+    this torch can."""
+    global _raw_stream
+    if stream is not None:
+        return stream.cuda_stream
+    if _raw_stream is None:
+        import torch
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+            lambda d: torch.cuda.current_stream(d).cuda_stream)
+    return _raw_stream(t.get_device())
+
+
 def _dev(t, name, dtype=None):
     import torch
     if not isinstance(t, torch.Tensor):
@@ -454,27 +471,27 @@ class Dispatch(NamedTuple):
 
 
 _TYPES = None
+_f32 = _i32 = _i64 = None
 
 
-def _types():
-    global _TYPES
-    if _TYPES is None:
-        import torch
-        _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
-    return _TYPES
+def _torch_types():
+    global _TYPES, _f32, _i32, _i64
+    import torch
+    _f32, _i32, _i64 = torch.float32, torch.int32, torch.int64
+    _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 
 def _rows(t, name):
     """(pointer, type, T, columns, row stride) of a matrix whose rows are
     contiguous and any distance apart."""
-    import torch
-    if not isinstance(t, torch.Tensor):
-        raise TypeError(f"{name} must be a torch tensor on the GPU")
-    if t.device.type != "cuda":
-        raise ValueError(f"{name} must live on a GPU (got {t.device})")
-    kind = _types().get(t.dtype)
+    if _TYPES is None:
+        _torch_types()
+    kind = _TYPES.get(getattr(t, "dtype", None))
     if kind is None:
+        _dev(t, name)                  # no tensor, or not on a GPU
         raise TypeError(f"{name} must be float32, bfloat16 or float16 (got {t.dtype})")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must live on a GPU (got {t.device})")
     if t.dim() != 2:
         raise ValueError(f"{name} must be a matrix (got {t.dim()} dimensions)")
     T, C = t.shape
@@ -488,33 +505,30 @@ def _rows(t, name):
 
 def _vec(t, name, dtype, shape):
     """Pointer of a contiguous GPU tensor of this type and shape."""
-    p = _dev(t, name, dtype)
-    if tuple(t.shape) != shape:
-        raise ValueError(f"{name} must have shape {shape} (got {tuple(t.shape)})")
-    return p
+    try:
+        if t.dtype is dtype and t.shape == shape and t.is_cuda and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    _dev(t, name, dtype)
+    raise ValueError(f"{name} must have shape {tuple(shape)} (got {tuple(t.shape)})")
 
 
-class _On:
-    """Allocations made inside belong to the stream that the work runs on."""
-
-    def __init__(self, stream):
-        import torch
-        self.ctx = None if stream is None else torch.cuda.stream(stream)
-
-    def __enter__(self):
-        if self.ctx is not None:
-            self.ctx.__enter__()
-
-    def __exit__(self, *e):
-        if self.ctx is not None:
-            self.ctx.__exit__(*e)
-
-
-def _workspace(nbytes, device):
+def _new(t, stream, *specs):
+    """Uninitialised tensors beside t, of the given (shape, type)s; they belong to
+    the stream that the work runs on."""
+    if stream is None:
+        return [t.new_empty(shape, dtype=dtype) for shape, dtype in specs]
     import torch
+    with torch.cuda.stream(stream):
+        return [t.new_empty(shape, dtype=dtype) for shape, dtype in specs]
+
+
+def _workspace(t, stream, nbytes):
+    """(tensor to hold, pointer) of a call's workspace."""
     if nbytes == 0:
         return None, None
-    w = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    w, = _new(t, stream, ((nbytes + 3) // 4, _i32))
     return w, w.data_ptr()
 
 
@@ -522,31 +536,25 @@ def token_logprobs(logits, tokens=None, top=0, inv_temperature=1.0, out=None, st
     """bo_token_logprobs: logits [T, V] (fp32, bf16 or fp16 GPU tensor, rows
     any distance apart), tokens int64 [T] (negative: none) or None. Returns a
     TokenLogprobs; ``out`` takes one of the same shapes to write into."""
-    import torch
     lp, kind, T, V, stride = _rows(logits, "logits")
     top = int(top)
-    f32, i32, dev = torch.float32, torch.int32, logits.device
     if top < 0:
         raise ValueError("top must not be negative")
-    tp = None if tokens is None else _vec(tokens, "tokens", torch.int64, (T,))
-    L = lib()
-    with _On(stream):
-        if out is None:
-            out = TokenLogprobs(
-                torch.empty(T, dtype=f32, device=dev), torch.empty(T, dtype=i32, device=dev),
-                torch.empty(T, dtype=f32, device=dev), torch.empty((T, 2), dtype=f32, device=dev),
-                torch.empty((T, top), dtype=i32, device=dev),
-                torch.empty((T, top), dtype=f32, device=dev))
-            ptrs = [t.data_ptr() for t in out]
-        else:
-            ptrs = [_vec(t, n, d, s) for t, n, d, s in zip(
-                out, TokenLogprobs._fields, (f32, i32, f32, f32, i32, f32),
-                ((T,), (T,), (T,), (T, 2), (T, top), (T, top)))]
-        need = L.bo_token_logprobs_workspace(T, V, top)
-        ws, wp = _workspace(need, dev)
-        st = L.bo_token_logprobs(lp, kind, T, V, stride, tp, inv_temperature, top, *ptrs, wp, need,
-                                 _stream(stream))
-    _check(st, "bo_token_logprobs")
+    tp = None if tokens is None else _vec(tokens, "tokens", _i64, (T,))
+    specs = (((T,), _f32), ((T,), _i32), ((T,), _f32), ((T, 2), _f32), ((T, top), _i32),
+             ((T, top), _f32))
+    if out is None:
+        out = TokenLogprobs(*_new(logits, stream, *specs))
+        ptrs = [t.data_ptr() for t in out]
+    else:
+        ptrs = [_vec(t, n, d, s) for t, n, (s, d) in zip(out, TokenLogprobs._fields, specs)]
+    L = _lib or lib()
+    need = L.bo_token_logprobs_workspace(T, V, top)
+    ws, wp = _workspace(logits, stream, need)
+    st = L.bo_token_logprobs(lp, kind, T, V, stride, tp, inv_temperature, top, *ptrs, wp, need,
+                             _stream_of(logits, stream))
+    if st:
+        _check(st, "bo_token_logprobs")
     return out
 
 
@@ -555,28 +563,27 @@ def token_logprobs_grad(logits, tokens, stats, entropy, grad_logprob=None, grad_
     """bo_token_logprobs_grad: the gradient of the logits ([T, V], their type)
     from those of token_logprobs' outputs; ``stats`` and ``entropy`` as it
     returned them. ``out`` may be ``logits`` itself."""
-    import torch
     lp, kind, T, V, stride = _rows(logits, "logits")
-    f32 = torch.float32
-    tp = None if tokens is None else _vec(tokens, "tokens", torch.int64, (T,))
-    sp, ep = _vec(stats, "stats", f32, (T, 2)), _vec(entropy, "entropy", f32, (T,))
-    gl = None if grad_logprob is None else _vec(grad_logprob, "grad_logprob", f32, (T,))
-    gh = None if grad_entropy is None else _vec(grad_entropy, "grad_entropy", f32, (T,))
+    tp = None if tokens is None else _vec(tokens, "tokens", _i64, (T,))
+    sp, ep = _vec(stats, "stats", _f32, (T, 2)), _vec(entropy, "entropy", _f32, (T,))
+    gl = None if grad_logprob is None else _vec(grad_logprob, "grad_logprob", _f32, (T,))
+    gh = None if grad_entropy is None else _vec(grad_entropy, "grad_entropy", _f32, (T,))
     if (top_ids is None) != (grad_top is None):
         raise ValueError("top_ids and grad_top go together")
     top, ip, gp = 0, None, None
     if top_ids is not None:
         top = top_ids.shape[-1]
-        ip, gp = _vec(top_ids, "top_ids", torch.int32, (T, top)), _vec(grad_top, "grad_top", f32, (T, top))
+        ip, gp = _vec(top_ids, "top_ids", _i32, (T, top)), _vec(grad_top, "grad_top", _f32, (T, top))
     if out is None:
-        with _On(stream):
-            out = torch.empty((T, V), dtype=logits.dtype, device=logits.device)
+        out, = _new(logits, stream, ((T, V), logits.dtype))
     op, okind, oT, oV, ostride = _rows(out, "out")
     if (okind, oT, oV) != (kind, T, V):
         raise ValueError("out must have the logits' shape and type")
-    st = lib().bo_token_logprobs_grad(lp, kind, T, V, stride, tp, inv_temperature, sp, ep, gl, gh,
-                                      top, ip, gp, op, ostride, _stream(stream))
-    _check(st, "bo_token_logprobs_grad")
+    st = (_lib or lib()).bo_token_logprobs_grad(lp, kind, T, V, stride, tp, inv_temperature, sp, ep,
+                                                gl, gh, top, ip, gp, op, ostride,
+                                                _stream_of(logits, stream))
+    if st:
+        _check(st, "bo_token_logprobs_grad")
     return out
 
 
@@ -597,24 +604,22 @@ def route(logits, top, bias=None, score="softmax", groups=1, top_groups=1, group
     is limited to the ``top_groups`` best groups, by the sum of their
     ``group_best`` largest values. Returns a Routing; ``out`` takes one of the
     same shapes to write into."""
-    import torch
     lp, kind, T, E, stride = _rows(logits, "logits")
     top = int(top)
     if top < 1:
         raise ValueError("top must be at least 1")
     sc = _score(score)
-    bp = None if bias is None else _vec(bias, "bias", torch.float32, (E,))
+    bp = None if bias is None else _vec(bias, "bias", _f32, (E,))
+    shape = (T, top)
     if out is None:
-        with _On(stream):
-            out = Routing(torch.empty((T, top), dtype=torch.int32, device=logits.device),
-                          torch.empty((T, top), dtype=torch.float32, device=logits.device))
+        out = Routing(*_new(logits, stream, (shape, _i32), (shape, _f32)))
         ip, wp = out.ids.data_ptr(), out.weights.data_ptr()
     else:
-        ip = _vec(out[0], "ids", torch.int32, (T, top))
-        wp = _vec(out[1], "weights", torch.float32, (T, top))
-    st = lib().bo_route(lp, kind, T, E, stride, bp, sc, top, groups, top_groups, group_best,
-                        1 if renormalise else 0, scale, ip, wp, _stream(stream))
-    _check(st, "bo_route")
+        ip, wp = _vec(out[0], "ids", _i32, shape), _vec(out[1], "weights", _f32, shape)
+    st = (_lib or lib()).bo_route(lp, kind, T, E, stride, bp, sc, top, groups, top_groups, group_best,
+                                  1 if renormalise else 0, scale, ip, wp, _stream_of(logits, stream))
+    if st:
+        _check(st, "bo_route")
     return out
 
 
@@ -623,23 +628,22 @@ def route_grad(logits, ids, grad_weights, score="softmax", renormalise=True, sca
     """bo_route_grad: the gradient of route's logits ([T, E], their type) from
     that of its weights, for the ``ids`` it chose. ``out`` may be ``logits``
     itself."""
-    import torch
     lp, kind, T, E, stride = _rows(logits, "logits")
-    if not isinstance(ids, torch.Tensor) or ids.dim() != 2:
+    if getattr(ids, "ndim", 0) != 2:
         raise TypeError("ids must be an int32 matrix on the GPU")
     top = ids.shape[1]
-    ip = _vec(ids, "ids", torch.int32, (T, top))
-    gp = _vec(grad_weights, "grad_weights", torch.float32, (T, top))
+    ip = _vec(ids, "ids", _i32, (T, top))
+    gp = _vec(grad_weights, "grad_weights", _f32, (T, top))
     sc = _score(score)
     if out is None:
-        with _On(stream):
-            out = torch.empty((T, E), dtype=logits.dtype, device=logits.device)
+        out, = _new(logits, stream, ((T, E), logits.dtype))
     op, okind, oT, oE, ostride = _rows(out, "out")
     if (okind, oT, oE) != (kind, T, E):
         raise ValueError("out must have the logits' shape and type")
-    st = lib().bo_route_grad(lp, kind, T, E, stride, sc, top, 1 if renormalise else 0, scale, ip,
-                             gp, op, ostride, _stream(stream))
-    _check(st, "bo_route_grad")
+    st = (_lib or lib()).bo_route_grad(lp, kind, T, E, stride, sc, top, 1 if renormalise else 0, scale,
+                                       ip, gp, op, ostride, _stream_of(logits, stream))
+    if st:
+        _check(st, "bo_route_grad")
     return out
 
 
@@ -648,25 +652,24 @@ def dispatch(ids, experts, capacity=0, out=None, stream=None):
     row-major order) grouped by expert, at most ``capacity`` each when that is
     not 0. Returns a Dispatch; ``out`` takes one of the same shapes to write
     into."""
-    import torch
-    idp = _dev(ids, "ids", torch.int32)
-    N, E, i32, dev = ids.numel(), int(experts), torch.int32, ids.device
+    if _TYPES is None:
+        _torch_types()
+    idp = _vec(ids, "ids", _i32, getattr(ids, "shape", ()))
+    N, E = ids.numel(), int(experts)
     if E < 1:
         raise ValueError("experts must be at least 1")
-    L = lib()
-    with _On(stream):
-        if out is None:
-            out = Dispatch(torch.empty(E, dtype=i32, device=dev),
-                           torch.empty(E + 1, dtype=i32, device=dev),
-                           torch.empty(N, dtype=i32, device=dev), torch.empty_like(ids))
-            ptrs = [t.data_ptr() for t in out]
-        else:
-            ptrs = [_vec(t, n, i32, s) for t, n, s in zip(
-                out, Dispatch._fields, ((E,), (E + 1,), (N,), tuple(ids.shape)))]
-        need = L.bo_dispatch_workspace(N, E)
-        ws, wp = _workspace(need, dev)
-        st = L.bo_dispatch(idp, N, E, capacity, *ptrs, wp, need, _stream(stream))
-    _check(st, "bo_dispatch")
+    specs = (((E,), _i32), ((E + 1,), _i32), ((N,), _i32), (ids.shape, _i32))
+    if out is None:
+        out = Dispatch(*_new(ids, stream, *specs))
+        ptrs = [t.data_ptr() for t in out]
+    else:
+        ptrs = [_vec(t, n, d, s) for t, n, (s, d) in zip(out, Dispatch._fields, specs)]
+    L = _lib or lib()
+    need = L.bo_dispatch_workspace(N, E)
+    ws, wp = _workspace(ids, stream, need)
+    st = L.bo_dispatch(idp, N, E, capacity, *ptrs, wp, need, _stream_of(ids, stream))
+    if st:
+        _check(st, "bo_dispatch")
     return out
 
 
