@@ -39,18 +39,6 @@ constexpr int kMergeAt = 32;             // candidates that are worth a merge
 // as the sums. The entropy loses 16 units of its last place at most.
 constexpr float kSlack = 16.0f;
 
-// max of three; NaN operands are dropped (a signalling one may come through)
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float d;
-  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
-  return d;
-}
-__device__ __forceinline__ float max2(float a, float b) {
-  float d;
-  asm("v_max_f32 %0, %1, %2" : "=v"(d) : "v"(a), "v"(b));
-  return d;
-}
-
 // The largest fp32 value below v (v finite or +inf).
 __device__ __forceinline__ float below(float v) {
   const unsigned u = __float_as_uint(v + 0.0f);

@@ -11,6 +11,7 @@
 // exchange lists by halves (the larger of a_i and b_{K-1-i} are the K best of
 // two falling lists, and form a bitonic sequence that log2 K steps sort).
 #include <algorithm>
+#include <type_traits>
 
 #include "serving.h"
 
@@ -115,21 +116,59 @@ __device__ __forceinline__ void join_lists(double* a) {
   keep_best<K, K>(a, b);
 }
 
+// A lane's `span` elements of a row of E from `first` on, -inf past the end.
+// Every lane loads (a load that only some lanes make waits for the one before
+// it): what would reach past the row starts earlier and is moved up.
+template <int TYPE>
+__device__ __forceinline__ void load_span(Vec<TYPE> (&q)[kSpan / Vec<TYPE>::kVec],
+                                          const typename Elem<TYPE>::T* x, int first, int span, int E) {
+  constexpr int KV = Vec<TYPE>::kVec;
+  if (E >= KV) {
+#pragma unroll
+    for (int p = 0; p < kSpan / KV; ++p)
+      if (p * KV < span) q[p].load(x + min(first + p * KV, E - KV));
+#pragma unroll
+    for (int p = 0; p < kSpan / KV; ++p) {
+      if (p * KV < span) {
+        const int past = first + p * KV - (E - KV);
+        if (__any(past > 0)) q[p].drop(max(past, 0));
+      } else {
+        q[p].fill_masked();
+      }
+    }
+  } else {
+#pragma unroll
+    for (int p = 0; p < kSpan / KV; ++p) q[p].fill_masked();
+    if (first == 0) q[0].load_part(x, E);
+  }
+}
+
 // Expert j's place in LDS: a gap after every 32 keeps lanes that walk groups of
 // 32 off one another's bank.
 __device__ __forceinline__ int at_of(int j) { return j + (j >> 5); }
 
-// 1 << shift lanes a row.
-template <int TYPE, int K, bool GROUPED>
-__global__ __launch_bounds__(kWg) void k_route(RouteArgs a, int shift) {
+// The larger two of a falling pair and of another.
+__device__ __forceinline__ void top_two(float& b1, float& b2, float o1, float o2) {
+  b2 = max2(b2 < o2 ? o2 : b2, b1 < o1 ? b1 : o1);
+  b1 = max2(b1, o1);
+}
+
+// How the groups lie: none (or none dropped), each of whole eights, or anyhow.
+enum { kNoGroups, kBlockGroups, kAnyGroups };
+
+// 1 << shift lanes a row. `div` is 65536 / eights per group, rounded up
+// (kBlockGroups): eight / (eights per group) = eight * div >> 16 for up to 128.
+template <int TYPE, int K, int GROUPS>
+__global__ __launch_bounds__(kWg) void k_route(RouteArgs a, int shift, int div) {
   using El = Elem<TYPE>;
   using V = Vec<TYPE>;
-  constexpr int kBlocks = kSpan / 8, kParts = 8 / V::kVec;
-  // a wave's rows: values and groups' codes; choices and what they weigh
-  __shared__ float lds_val[GROUPED ? kWg / 64 : 1][GROUPED ? 64 * (kSpan + 1) : 1];
-  __shared__ unsigned lds_grp[GROUPED ? kWg / 64 : 1][GROUPED ? 64 * kSpan / 2 : 1];
-  __shared__ int lds_id[kWg / 64][64 * K];
-  __shared__ float lds_w[kWg / 64][64 * K];
+  constexpr int kBlocks = kSpan / 8;
+  // per wave: choices and what they weigh, and before them the groups' work
+  constexpr int kChoice = 2 * 64 * K;
+  constexpr int kGroup = GROUPS == kNoGroups ? 0 : GROUPS == kBlockGroups ? 64 * kBlocks * 3 + 64 * kBlocks
+                                                                         : 64 * (kSpan + 1) + 64 * kSpan / 2;
+  __shared__ float lds[kWg / 64][kChoice > kGroup ? kChoice : kGroup];
+  __shared__ alignas(16) float lds_bias[BO_MAX_EXPERTS + 8 * kSpan];
   const auto fmax2 = [](float p, float q) { return fmaxf(p, q); };
   const auto fadd2 = [](float p, float q) { return p + q; };
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -137,20 +176,19 @@ __global__ __launch_bounds__(kWg) void k_route(RouteArgs a, int shift) {
   // experts a lane holds: whole eights, consecutive ones
   const int span = ((((a.E + 7) >> 3) + lpt - 1) >> shift) << 3;
   const int first = sub * span;
+  const bool scored = GROUPS != kNoGroups || a.bias;      // else the logits are compared
+  if (a.bias) {
+    for (int j = threadIdx.x; j < span * lpt; j += kWg) lds_bias[j] = j < a.E ? a.bias[j] : kNegInf;
+    __syncthreads();
+  }
   const int64_t step = (int64_t)gridDim.x * (kWg / 64) * rows;
   for (int64_t base = (int64_t)blockIdx.x * (kWg / 64) * rows; base < a.T; base += step) {
     const int64_t row = base + wave * rows + slot;
     const bool live = row < a.T;
     const typename El::T* x =
         static_cast<const typename El::T*>(a.logits) + (live ? row : 0) * a.stride;
-    V q[kBlocks * kParts];
-#pragma unroll
-    for (int p = 0; p < kBlocks * kParts; ++p) {
-      const int j = first + p * V::kVec;
-      if (p * V::kVec >= span || j >= a.E) q[p].fill_masked();
-      else if (j + V::kVec <= a.E) q[p].load(x + j);
-      else q[p].load_part(x + j, a.E - j);
-    }
+    V q[kSpan / V::kVec];
+    load_span<TYPE>(q, x, first, span, a.E);
     const auto logit = [&](int i) { return q[i / V::kVec].get(i % V::kVec); };
     // softmax statistics; a row with a NaN or +inf has no choice
     float m = 0.0f, inv = 1.0f;
@@ -158,18 +196,26 @@ __global__ __launch_bounds__(kWg) void k_route(RouteArgs a, int shift) {
     if (a.score == BO_SCORE_SOFTMAX) {
       m = kNegInf;
 #pragma unroll
-      for (int i = 0; i < kSpan; ++i) {
-        m = fmaxf(m, logit(i));
-        bad = bad || __builtin_isnan(logit(i));
-      }
+      for (int b = 0; b < kBlocks; ++b)
+        if (8 * b < span) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            m = max2(m, logit(8 * b + e));
+            bad = bad || __builtin_isnan(logit(8 * b + e));
+          }
+        }
       m = row_reduce(m, lpt, fmax2);
       bad = bad || m == __builtin_huge_valf();
       bad = (__ballot(bad) >> (slot << shift) & (~0ull >> (64 - lpt))) != 0;
       m = m == kNegInf ? 0.0f : m;
-      if (GROUPED || a.bias || !a.renorm) {
+      if (scored || !a.renorm) {
         float t = 0.0f;
 #pragma unroll
-        for (int i = 0; i < kSpan; ++i) t += __builtin_amdgcn_exp2f((logit(i) - m) * kLog2e);
+        for (int b = 0; b < kBlocks; ++b)
+          if (8 * b < span) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) t += __builtin_amdgcn_exp2f((logit(8 * b + e) - m) * kLog2e);
+          }
         inv = 1.0f / row_reduce(t, lpt, fadd2);
       }
     }
@@ -182,7 +228,7 @@ __global__ __launch_bounds__(kWg) void k_route(RouteArgs a, int shift) {
     const auto values = [&](int b, float (&v)[8]) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = logit(8 * b + e);
-      if (GROUPED || a.bias) {
+      if (scored) {
         if (a.score == BO_SCORE_SIGMOID) {
 #pragma unroll
           for (int e = 0; e < 8; ++e)
@@ -192,16 +238,10 @@ __global__ __launch_bounds__(kWg) void k_route(RouteArgs a, int shift) {
           for (int e = 0; e < 8; ++e) v[e] = __builtin_amdgcn_exp2f((v[e] - m) * kLog2e) * inv;
         }
         if (a.bias) {
-#pragma unroll
-          for (int p = 0; p < 2; ++p) {
-            Vec<BO_TYPE_F32> t;
-            const int j = first + 8 * b + 4 * p;
-            if (j >= a.E) t.fill_masked();
-            else if (j + 4 <= a.E) t.load(a.bias + j);
-            else t.load_part(a.bias + j, a.E - j);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[4 * p + e] += t.get(e);
-          }
+          const float4* t = reinterpret_cast<const float4*>(lds_bias + first + 8 * b);
+          const float4 lo = t[0], hi = t[1];
+          v[0] += lo.x; v[1] += lo.y; v[2] += lo.z; v[3] += lo.w;
+          v[4] += hi.x; v[5] += hi.y; v[6] += hi.z; v[7] += hi.w;
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = logit(8 * b + e) > kNegInf ? v[e] : kNegInf;
@@ -209,10 +249,59 @@ __global__ __launch_bounds__(kWg) void k_route(RouteArgs a, int shift) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = fmaxf(v[e], kNegInf);     // a NaN is no choice
     };
-    float* val = GROUPED ? lds_val[wave] + slot * lpt * (kSpan + 1) : nullptr;
-    if constexpr (GROUPED) {
+    float kept[GROUPS == kBlockGroups ? kSpan : 1];
+    float* val = lds[wave] + slot * lpt * (kSpan + 1);
+    // a group that top_groups or more come before is dropped
+    const auto dropped = [&](const unsigned* grp, int g) {
+      const unsigned mine = grp[g];
+      int before = 0;
+      for (int o = 0; o < a.groups; ++o) before += grp[o] > mine || (grp[o] == mine && o < g);
+      return before >= a.top_groups;
+    };
+    if constexpr (GROUPS == kBlockGroups) {
+      // the best two of each eight, then of each group
+      float2* two = reinterpret_cast<float2*>(lds[wave]) + slot * lpt * kBlocks;
+      unsigned* grp = reinterpret_cast<unsigned*>(lds[wave] + 64 * kBlocks * 2) + slot * lpt * kBlocks;
+      unsigned* drop = grp + 64 * kBlocks;
+      const int eights = a.E / a.groups / 8, at = first >> 3;
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b)
+        if (8 * b < span) {
+          float v[8];
+          values(b, v);
+          float b1 = kNegInf, b2 = kNegInf;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            kept[8 * b + e] = v[e];
+            b2 = __builtin_amdgcn_fmed3f(b1, b2, v[e]);
+            b1 = max2(b1, v[e]);
+          }
+          two[at + b] = make_float2(b1, b2);
+        }
+      __syncthreads();
+      for (int g = sub; g < a.groups; g += lpt) {
+        float2 best = two[g * eights];
+        for (int e = 1; e < eights; ++e) top_two(best.x, best.y, two[g * eights + e].x, two[g * eights + e].y);
+        grp[g] = code_of(a.group_best == 2 ? best.x + best.y : best.x);
+      }
+      __syncthreads();
+      for (int g = sub; g < a.groups; g += lpt) drop[g] = dropped(grp, g);
+      __syncthreads();
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b)
+        if (8 * b < span) {
+          const bool out = drop[min((at + b) * div >> 16, a.groups - 1)];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float v = !a.bias && kept[8 * b + e] > kNegInf ? logit(8 * b + e) : kept[8 * b + e];
+            kept[8 * b + e] = out ? kNegInf : v;
+          }
+        }
+      __syncthreads();                      // (the choices take this memory's place)
+    }
+    if constexpr (GROUPS == kAnyGroups) {
       const int per = a.E / a.groups;
-      unsigned* grp = lds_grp[wave] + slot * lpt * (kSpan / 2);
+      unsigned* grp = reinterpret_cast<unsigned*>(lds[wave] + 64 * (kSpan + 1)) + slot * lpt * (kSpan / 2);
 #pragma unroll
       for (int b = 0; b < kBlocks; ++b)
         if (8 * b < span) {
@@ -224,22 +313,13 @@ __global__ __launch_bounds__(kWg) void k_route(RouteArgs a, int shift) {
       __syncthreads();
       for (int g = sub; g < a.groups; g += lpt) {
         float b1 = kNegInf, b2 = kNegInf;
-        for (int e = g * per; e < (g + 1) * per; ++e) {
-          const float t = val[at_of(e)];
-          b2 = fmaxf(b2, fminf(b1, t));
-          b1 = fmaxf(b1, t);
-        }
+        for (int e = g * per; e < (g + 1) * per; ++e) top_two(b1, b2, val[at_of(e)], kNegInf);
         grp[g] = code_of(a.group_best == 2 ? b1 + b2 : b1);
       }
       __syncthreads();
-      // a group that top_groups or more come before is dropped
-      for (int g = sub; g < a.groups; g += lpt) {
-        const unsigned mine = grp[g];
-        int before = 0;
-        for (int o = 0; o < a.groups; ++o) before += grp[o] > mine || (grp[o] == mine && o < g);
-        if (before >= a.top_groups)
+      for (int g = sub; g < a.groups; g += lpt)
+        if (dropped(grp, g))
           for (int e = g * per; e < (g + 1) * per; ++e) val[at_of(e)] = kNegInf;
-      }
       __syncthreads();
     }
     // the lane's best
@@ -251,7 +331,10 @@ __global__ __launch_bounds__(kWg) void k_route(RouteArgs a, int shift) {
     for (int b = 0; b < kBlocks; ++b) {
       if (8 * b < span) {
         float v[8];
-        if constexpr (GROUPED) {
+        if constexpr (GROUPS == kBlockGroups) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = kept[8 * b + e];
+        } else if constexpr (GROUPS == kAnyGroups) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
             v[e] = val[at_of(first + 8 * b) + e];
@@ -285,9 +368,10 @@ __global__ __launch_bounds__(kWg) void k_route(RouteArgs a, int shift) {
     if (lpt > 4) join_lists<K, 4>(best);
     if (lpt > 8) join_lists<K, 8>(best);
     if (lpt > 16) join_lists<K, 16>(best);
+    if constexpr (GROUPS == kAnyGroups) __syncthreads();
     // weights: lane `sub` takes choices sub, sub + lpt, ..
-    int* cid = lds_id[wave] + slot * K;
-    float* cw = lds_w[wave] + slot * K;
+    int* cid = reinterpret_cast<int*>(lds[wave]) + slot * K;
+    float* cw = lds[wave] + 64 * K + slot * K;
     if (sub == 0) {
 #pragma unroll
       for (int i = 0; i < K; ++i) {
@@ -334,8 +418,9 @@ __global__ __launch_bounds__(kWg) void k_route(RouteArgs a, int shift) {
 
 // The same lanes hold a row: each choice's term goes to its expert's place in
 // LDS, then every lane adds the dense part (softmax, not renormalised: -scale
-// s_j sum_k s_k g_k) to its experts' and writes them.
-template <int TYPE>
+// s_j sum_k s_k g_k) to its experts' and writes them. K >= top choices, of
+// which a lane takes sub, sub + lpt, ..
+template <int TYPE, int K>
 __global__ __launch_bounds__(kWg) void k_route_grad(RouteGradArgs a, int shift) {
   using El = Elem<TYPE>;
   using V = Vec<TYPE>;
@@ -355,27 +440,40 @@ __global__ __launch_bounds__(kWg) void k_route_grad(RouteGradArgs a, int shift) 
     const bool live = row < a.T;
     const int64_t r = live ? row : 0;
     const typename El::T* x = static_cast<const typename El::T*>(a.logits) + r * a.stride;
-    const int32_t* ids = a.ids + r * a.top;
-    const float* g = a.g + r * a.top;
+    // a lane's choices: expert, logit, the weight's gradient
+    int id[K];
+    float l[K], g[K];
+#pragma unroll
+    for (int t = 0; t < K; ++t)
+      if (t * lpt < a.top) {
+        const int n = min(t * lpt + sub, a.top - 1);
+        id[t] = a.ids[r * a.top + n];
+        g[t] = a.g[r * a.top + n];
+        if (id[t] >= a.E || t * lpt + sub >= a.top) id[t] = -1;
+      }
+#pragma unroll
+    for (int t = 0; t < K; ++t)
+      if (t * lpt < a.top) l[t] = El::load(x[max(id[t], 0)]);
     V q[kParts];
     float m = 0.0f, inv = 1.0f;
     if (dense) {
-#pragma unroll
-      for (int p = 0; p < kParts; ++p) {
-        const int j = first + p * V::kVec;
-        if (p * V::kVec >= span || j >= a.E) q[p].fill_masked();
-        else if (j + V::kVec <= a.E) q[p].load(x + j);
-        else q[p].load_part(x + j, a.E - j);
-      }
+      load_span<TYPE>(q, x, first, span, a.E);
       m = kNegInf;
 #pragma unroll
-      for (int i = 0; i < kSpan; ++i) m = fmaxf(m, q[i / V::kVec].get(i % V::kVec));
+      for (int p = 0; p < kParts; ++p)
+        if (p * V::kVec < span) {
+#pragma unroll
+          for (int e = 0; e < V::kVec; ++e) m = max2(m, q[p].get(e));
+        }
       m = row_reduce(m, lpt, fmax2);
       m = m == kNegInf ? 0.0f : m;
       float t = 0.0f;
 #pragma unroll
-      for (int i = 0; i < kSpan; ++i)
-        t += __builtin_amdgcn_exp2f((q[i / V::kVec].get(i % V::kVec) - m) * kLog2e);
+      for (int p = 0; p < kParts; ++p)
+        if (p * V::kVec < span) {
+#pragma unroll
+          for (int e = 0; e < V::kVec; ++e) t += __builtin_amdgcn_exp2f((q[p].get(e) - m) * kLog2e);
+        }
       inv = 1.0f / row_reduce(t, lpt, fadd2);
     }
 #pragma unroll
@@ -384,64 +482,65 @@ __global__ __launch_bounds__(kWg) void k_route_grad(RouteGradArgs a, int shift) 
 #pragma unroll
         for (int e = 0; e < 8; ++e) term[at_of(first + 8 * b) + e] = 0.0f;
       }
-    __syncthreads();
     const auto sigm = [](float t) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-t * kLog2e)); };
     float hi = kNegInf, any = 0.0f;
-    for (int n = sub; n < a.top; n += lpt) {
-      const int id = ids[n];
-      if (id >= 0 && id < a.E) {
-        hi = fmaxf(hi, El::load(x[id]));
-        any = 1.0f;
+#pragma unroll
+    for (int t = 0; t < K; ++t)
+      if (t * lpt < a.top) {
+        hi = id[t] >= 0 ? fmaxf(hi, l[t]) : hi;
+        any = id[t] >= 0 ? 1.0f : any;
       }
+    if (a.renorm) {
+      hi = row_reduce(hi, lpt, fmax2);
+      if (!softmax) hi = fminf(hi, 0.0f);
     }
     any = row_reduce(any, lpt, fmax2);
-    hi = row_reduce(hi, lpt, fmax2);
-    if (!softmax) hi = fminf(hi, 0.0f);
     // the weights before their common factor, as in the forward pass
-    const auto weight = [&](float l) {
-      if (dense) return __builtin_amdgcn_exp2f((l - m) * kLog2e) * inv;
-      if (!a.renorm) return sigm(l);
-      if (!softmax && l > 0.0f) return sigm(l);
-      const float w = __builtin_amdgcn_exp2f((l - hi) * kLog2e);
-      return softmax ? w : w * sigm(-l);
+    const auto weight = [&](float t) {
+      if (dense) return __builtin_amdgcn_exp2f((t - m) * kLog2e) * inv;
+      if (!a.renorm) return sigm(t);
+      if (!softmax && t > 0.0f) return sigm(t);
+      const float w = __builtin_amdgcn_exp2f((t - hi) * kLog2e);
+      return softmax ? w : w * sigm(-t);
     };
-    float total = 0.0f, wg = 0.0f;
-    for (int n = sub; n < a.top; n += lpt) {
-      const int id = ids[n];
-      if (id >= 0 && id < a.E) {
-        const float w = weight(El::load(x[id]));
-        total += w;
-        wg = fmaf(w, g[n], wg);
+    float total = 0.0f, wg = 0.0f, w[K];
+#pragma unroll
+    for (int t = 0; t < K; ++t)
+      if (t * lpt < a.top) {
+        w[t] = id[t] >= 0 ? weight(l[t]) : 0.0f;
+        total += w[t];
+        if (id[t] >= 0) wg = fmaf(w[t], g[t], wg);
       }
-    }
-    total = row_reduce(total, lpt, fadd2);
-    wg = row_reduce(wg, lpt, fadd2);
+    if (a.renorm) total = row_reduce(total, lpt, fadd2);
+    if (a.renorm || dense) wg = row_reduce(wg, lpt, fadd2);
     const float norm = a.renorm ? 1.0f / total : 1.0f, mean = a.renorm ? wg * norm : 0.0f;
-    for (int n = sub; n < a.top; n += lpt) {
-      const int id = ids[n];
-      if (id >= 0 && id < a.E) {
-        const float l = El::load(x[id]);
-        float d = a.scale * (weight(l) * norm) * (g[n] - mean);
-        if (!softmax) d *= sigm(-l);
-        term[at_of(id)] = d;
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < K; ++t)
+      if (t * lpt < a.top && id[t] >= 0) {
+        const float d = a.scale * (w[t] * norm) * (g[t] - mean);
+        term[at_of(id[t])] = softmax ? d : d * sigm(-l[t]);
       }
-    }
     __syncthreads();
     typename El::T* out = static_cast<typename El::T*>(a.out) + r * a.out_stride;
     const float back = dense && any > 0.0f ? -a.scale * wg * inv : 0.0f;
 #pragma unroll
     for (int p = 0; p < kParts; ++p) {
       const int j = first + p * V::kVec;
-      if (p * V::kVec < span && j < a.E && live) {
+      if (p * V::kVec < span) {
         float v[V::kVec];
 #pragma unroll
-        for (int e = 0; e < V::kVec; ++e) {
-          v[e] = term[at_of(j) + e];
-          if (back != 0.0f) v[e] = fmaf(back, __builtin_amdgcn_exp2f((q[p].get(e) - m) * kLog2e), v[e]);
+        for (int e = 0; e < V::kVec; ++e) v[e] = term[at_of(j) + e];
+        if (dense) {
+#pragma unroll
+          for (int e = 0; e < V::kVec; ++e) {
+            const float s = __builtin_amdgcn_exp2f((q[p].get(e) - m) * kLog2e);
+            v[e] = back != 0.0f ? fmaf(back, s, v[e]) : v[e];
+          }
         }
         q[p].set_all(v);
-        if (j + V::kVec <= a.E) q[p].store(out + j);
-        else q[p].store_part(out + j, a.E - j);
+        if (live && j + V::kVec <= a.E) q[p].store(out + j);
+        else if (live && j < a.E) q[p].store_part(out + j, a.E - j);
       }
     }
     __syncthreads();
@@ -459,21 +558,38 @@ unsigned row_blocks(int64_t T, int shift) {
   return static_cast<unsigned>(std::min<int64_t>((T + rows - 1) / rows, 1 << 20));
 }
 
-template <int TYPE, int K>
-void launch_choice(const RouteArgs& a, int shift, unsigned grid, hipStream_t st) {
-  if (a.groups > 1 && a.top_groups < a.groups) k_route<TYPE, K, true><<<grid, kWg, 0, st>>>(a, shift);
-  else k_route<TYPE, K, false><<<grid, kWg, 0, st>>>(a, shift);
+// What fits the smallest list of at least `top`.
+template <typename F>
+void by_top(int top, F f) {
+  if (top <= 2) f(std::integral_constant<int, 2>());
+  else if (top <= 4) f(std::integral_constant<int, 4>());
+  else if (top <= 8) f(std::integral_constant<int, 8>());
+  else if (top <= 16) f(std::integral_constant<int, 16>());
+  else f(std::integral_constant<int, 32>());
 }
 
 template <int TYPE>
 hipError_t launch_typed(const RouteArgs& a, hipStream_t st) {
   const int shift = lanes_shift(a.E);
   const unsigned grid = row_blocks(a.T, shift);
-  if (a.top <= 2) launch_choice<TYPE, 2>(a, shift, grid, st);
-  else if (a.top <= 4) launch_choice<TYPE, 4>(a, shift, grid, st);
-  else if (a.top <= 8) launch_choice<TYPE, 8>(a, shift, grid, st);
-  else if (a.top <= 16) launch_choice<TYPE, 16>(a, shift, grid, st);
-  else launch_choice<TYPE, 32>(a, shift, grid, st);
+  const int per = a.E / a.groups, eights = per / 8;
+  by_top(a.top, [&](auto k) {
+    constexpr int K = decltype(k)::value;
+    if (a.groups == 1 || a.top_groups == a.groups)
+      k_route<TYPE, K, kNoGroups><<<grid, kWg, 0, st>>>(a, shift, 0);
+    else if (per % 8 == 0)
+      k_route<TYPE, K, kBlockGroups><<<grid, kWg, 0, st>>>(a, shift, (65536 + eights - 1) / eights);
+    else
+      k_route<TYPE, K, kAnyGroups><<<grid, kWg, 0, st>>>(a, shift, 0);
+  });
+  return hipGetLastError();
+}
+
+template <int TYPE>
+hipError_t launch_typed(const RouteGradArgs& a, hipStream_t st) {
+  const int shift = lanes_shift(a.E);
+  const unsigned grid = row_blocks(a.T, shift);
+  by_top(a.top, [&](auto k) { k_route_grad<TYPE, decltype(k)::value><<<grid, kWg, 0, st>>>(a, shift); });
   return hipGetLastError();
 }
 
@@ -486,12 +602,9 @@ hipError_t launch_route(const RouteArgs& a, hipStream_t st) {
 }
 
 hipError_t launch_route_grad(const RouteGradArgs& a, hipStream_t st) {
-  const int shift = lanes_shift(a.E);
-  const unsigned grid = row_blocks(a.T, shift);
-  if (a.type == BO_TYPE_F32) k_route_grad<BO_TYPE_F32><<<grid, kWg, 0, st>>>(a, shift);
-  else if (a.type == BO_TYPE_BF16) k_route_grad<BO_TYPE_BF16><<<grid, kWg, 0, st>>>(a, shift);
-  else k_route_grad<BO_TYPE_F16><<<grid, kWg, 0, st>>>(a, shift);
-  return hipGetLastError();
+  if (a.type == BO_TYPE_F32) return launch_typed<BO_TYPE_F32>(a, st);
+  if (a.type == BO_TYPE_BF16) return launch_typed<BO_TYPE_BF16>(a, st);
+  return launch_typed<BO_TYPE_F16>(a, st);
 }
 
 }  // namespace bo

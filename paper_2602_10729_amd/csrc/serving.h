@@ -66,6 +66,27 @@ struct Vec {
         }
       }
   }
+  // Drops the first n elements and fills with -inf from behind (n >= 0; all of
+  // them from kVec on).
+  __device__ __forceinline__ void drop(int n) {
+    const uint32_t b = bits_of(Elem<TYPE>::store(-__builtin_huge_valf()));
+    const uint32_t f = kVec == 4 ? b : b | (b << 16);
+    if constexpr (kVec == 8) {
+      const bool one = n & 1;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t s = __builtin_amdgcn_alignbit(i < 3 ? q[i + 1] : f, q[i], 16);
+        q[i] = one ? s : q[i];
+      }
+      n >>= 1;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q[i] = (n & 1) ? (i < 3 ? q[i + 1] : f) : q[i];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q[i] = (n & 2) ? (i < 2 ? q[i + 2] : f) : q[i];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q[i] = n >= 4 ? f : q[i];
+  }
   __device__ __forceinline__ void fill_masked() {
     const uint32_t b = bits_of(Elem<TYPE>::store(-__builtin_huge_valf()));
 #pragma unroll
@@ -124,6 +145,18 @@ __device__ __forceinline__ float key_value(unsigned long long k) {
 }
 __device__ __forceinline__ int key_index(unsigned long long k) {
   return static_cast<int>(0xFFFFFFFFu - static_cast<unsigned>(k));
+}
+
+// max of three; NaN operands are dropped (a signalling one may come through)
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
+  return d;
+}
+__device__ __forceinline__ float max2(float a, float b) {
+  float d;
+  asm("v_max_f32 %0, %1, %2" : "=v"(d) : "v"(a), "v"(b));
+  return d;
 }
 
 inline size_t type_bytes(int type) { return type == BO_TYPE_F32 ? 4 : 2; }
