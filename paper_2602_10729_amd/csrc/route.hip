@@ -22,6 +22,7 @@ constexpr int kWg = 256;
 constexpr float kNegInf = -__builtin_huge_valf();
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr int kSpan = 32;                    // experts a lane holds
+constexpr int64_t kLanesWanted = 4096 * 64;  // four waves on every SIMD
 constexpr unsigned kExpTwo52 = 0x43300000u;  // high word of 2^52
 
 // ---- keys -----------------------------------------------------------------
@@ -147,6 +148,9 @@ __device__ __forceinline__ void load_span(Vec<TYPE> (&q)[kSpan / Vec<TYPE>::kVec
 // 32 off one another's bank.
 __device__ __forceinline__ int at_of(int j) { return j + (j >> 5); }
 
+// LDS words of a row of n places.
+__host__ __device__ constexpr int row_words(int n) { return n + (n >> 5) + 1; }
+
 // The larger two of a falling pair and of another.
 __device__ __forceinline__ void top_two(float& b1, float& b2, float o1, float o2) {
   b2 = max2(b2 < o2 ? o2 : b2, b1 < o1 ? b1 : o1);
@@ -159,7 +163,7 @@ enum { kNoGroups, kBlockGroups, kAnyGroups };
 // 1 << shift lanes a row. `div` is 65536 / eights per group, rounded up
 // (kBlockGroups): eight / (eights per group) = eight * div >> 16 for up to 128.
 template <int TYPE, int K, int GROUPS>
-__global__ __launch_bounds__(kWg) void k_route(RouteArgs a, int shift, int div) {
+__global__ __launch_bounds__(kWg, K <= 8 && GROUPS != kAnyGroups ? 4 : 1) void k_route(RouteArgs a, int shift, int div) {
   using El = Elem<TYPE>;
   using V = Vec<TYPE>;
   constexpr int kBlocks = kSpan / 8;
@@ -425,7 +429,7 @@ __global__ __launch_bounds__(kWg) void k_route_grad(RouteGradArgs a, int shift) 
   using El = Elem<TYPE>;
   using V = Vec<TYPE>;
   constexpr int kParts = kSpan / V::kVec;
-  __shared__ float lds_term[kWg / 64][64 * (kSpan + 1)];
+  extern __shared__ float lds_term[];       // [waves][rows][row_words]
   const auto fmax2 = [](float p, float q) { return fmaxf(p, q); };
   const auto fadd2 = [](float p, float q) { return p + q; };
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -434,7 +438,7 @@ __global__ __launch_bounds__(kWg) void k_route_grad(RouteGradArgs a, int shift) 
   const int first = sub * span;
   const int64_t step = (int64_t)gridDim.x * (kWg / 64) * rows;
   const bool softmax = a.score == BO_SCORE_SOFTMAX, dense = softmax && !a.renorm;
-  float* term = lds_term[wave] + slot * lpt * (kSpan + 1);
+  float* term = lds_term + (wave * rows + slot) * row_words(span << shift);
   for (int64_t base = (int64_t)blockIdx.x * (kWg / 64) * rows; base < a.T; base += step) {
     const int64_t row = base + wave * rows + slot;
     const bool live = row < a.T;
@@ -547,10 +551,12 @@ __global__ __launch_bounds__(kWg) void k_route_grad(RouteGradArgs a, int shift) 
   }
 }
 
-// As few lanes a row as hold it.
-int lanes_shift(int E) {
+// As few lanes a row as hold it; more, down to eight experts each, while that
+// leaves the chip short of waves.
+int lanes_shift(int64_t T, int E) {
   int shift = 0;
   while ((kSpan << shift) < E) ++shift;
+  while ((8 << shift) < E && shift < 5 && (T << shift) < kLanesWanted) ++shift;
   return shift;
 }
 unsigned row_blocks(int64_t T, int shift) {
@@ -570,7 +576,7 @@ void by_top(int top, F f) {
 
 template <int TYPE>
 hipError_t launch_typed(const RouteArgs& a, hipStream_t st) {
-  const int shift = lanes_shift(a.E);
+  const int shift = lanes_shift(a.T, a.E);
   const unsigned grid = row_blocks(a.T, shift);
   const int per = a.E / a.groups, eights = per / 8;
   by_top(a.top, [&](auto k) {
@@ -587,9 +593,11 @@ hipError_t launch_typed(const RouteArgs& a, hipStream_t st) {
 
 template <int TYPE>
 hipError_t launch_typed(const RouteGradArgs& a, hipStream_t st) {
-  const int shift = lanes_shift(a.E);
+  const int shift = lanes_shift(a.T, a.E);
   const unsigned grid = row_blocks(a.T, shift);
-  by_top(a.top, [&](auto k) { k_route_grad<TYPE, decltype(k)::value><<<grid, kWg, 0, st>>>(a, shift); });
+  const int span = ((((a.E + 7) >> 3) + (1 << shift) - 1) >> shift) << 3;
+  const size_t lds = sizeof(float) * (kWg >> shift) * row_words(span << shift);
+  by_top(a.top, [&](auto k) { k_route_grad<TYPE, decltype(k)::value><<<grid, kWg, lds, st>>>(a, shift); });
   return hipGetLastError();
 }
 
