@@ -8,6 +8,9 @@
 // with a lane's expert are a mask, built from one ballot per bit of the
 // expert's number, and a pair's rank is the wave's count so far plus the lower
 // lanes of the mask. Counts of the waves of a tile are then summed in order.
+// A tile is put in order in LDS first, so that an expert's pairs are written in
+// runs (32 of a popular tile's 8192 over 256 experts) rather than four bytes
+// here and there: 23 -> 19 us for 2.1M pairs.
 // What fits one tile takes one launch. Nothing depends on the order in which
 // atomics arrive: they only add integers.
 #include <algorithm>
@@ -23,6 +26,9 @@ constexpr int kItems = 8;                 // pairs a lane holds
 constexpr int kTile = kWg * kItems;
 constexpr int kMaxBlocks = 256;
 
+// Words of a block's counts: whole 16-byte groups.
+__host__ __device__ constexpr int row_of(int E) { return (E + 3) & ~3; }
+
 __global__ __launch_bounds__(kWg) void k_dispatch_count(const int32_t* __restrict__ ids, int64_t N,
                                                         int64_t chunk, int E,
                                                         int32_t* __restrict__ hist) {
@@ -36,7 +42,8 @@ __global__ __launch_bounds__(kWg) void k_dispatch_count(const int32_t* __restric
     if (id >= 0 && id < E) atomicAdd(&cnt[id], 1);
   }
   __syncthreads();
-  if (threadIdx.x < E) hist[(int64_t)blockIdx.x * E + threadIdx.x] = cnt[threadIdx.x];
+  const int row = row_of(E);
+  if (threadIdx.x < row) hist[blockIdx.x * row + threadIdx.x] = threadIdx.x < E ? cnt[threadIdx.x] : 0;
 }
 
 // Thread e's `kept` summed over the threads before it. Two barriers.
@@ -56,7 +63,8 @@ __device__ int scan_before(int kept, int* wave_sum) {
   return before;
 }
 
-// Dynamic LDS: the waves' counts [kWaves][E].
+// Dynamic LDS: the waves' counts [kWaves][E]; unless ONE, the tile's places in
+// `order` and pairs, sorted by expert.
 template <bool ONE>
 __global__ __launch_bounds__(kWg) void k_dispatch_place(const int32_t* __restrict__ ids, int64_t N,
                                                         int64_t chunk, int E, int64_t capacity,
@@ -66,9 +74,12 @@ __global__ __launch_bounds__(kWg) void k_dispatch_place(const int32_t* __restric
                                                         int32_t* __restrict__ order,
                                                         int32_t* __restrict__ position) {
   extern __shared__ int32_t cnt[];
+  int32_t* places = cnt + kWaves * E;
+  uint16_t* pairs = reinterpret_cast<uint16_t*>(places + kTile);
   __shared__ int32_t all[BO_MAX_EXPERTS];     // pairs of an expert
   __shared__ int32_t seen[BO_MAX_EXPERTS];    // of them before this tile
   __shared__ int32_t start[BO_MAX_EXPERTS];   // where the expert's pairs begin
+  __shared__ int32_t slot0[BO_MAX_EXPERTS];   // its first slot in the tile, less `seen` before it
   __shared__ int wave_sum[kWaves];
   __shared__ int kept_total;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -94,29 +105,47 @@ __global__ __launch_bounds__(kWg) void k_dispatch_place(const int32_t* __restric
     all[tid] = 0;
     seen[tid] = 0;
   }
+  // a tile: wave after wave, 64 pairs at a time (past its end the last pair
+  // again); the first is on its way while the counts are summed
+  const int64_t p0 = blockIdx.x * chunk, p1 = min(N, p0 + chunk);
+  int id[kItems];
+  const auto fetch = [&](int64_t t0) {
+    const int n = static_cast<int>(min<int64_t>(kTile, p1 - t0)), items = (n + kWg - 1) / kWg;
+#pragma unroll
+    for (int i = 0; i < kItems; ++i)
+      if (i < items) id[i] = ids[t0 + min(wave * 64 * items + lane + 64 * i, n - 1)];
+  };
+  fetch(p0);
   __syncthreads();
   if (!ONE) {
-    // every thread sums some blocks' counts of one expert
-    int width = 64;
-    while (width < E) width <<= 1;
-    const int e = tid & (width - 1), parts = kWg / width;
-    int before = 0, total = 0;
+    // every thread sums some blocks' counts of four experts, all loads at once
+    const int quads = row_of(E) / 4;
+    int width = 16;
+    while (width < quads) width <<= 1;
+    const int e = (tid & (width - 1)) * 4, parts = kWg / width, nb = static_cast<int>(gridDim.x);
     if (e < E) {
-#pragma unroll 8
-      for (int b = tid / width; b < static_cast<int>(gridDim.x); b += parts) {
-        const int n = hist[b * E + e];
-        total += n;
-        before += b < static_cast<int>(blockIdx.x) ? n : 0;
+      const int4* rows = reinterpret_cast<const int4*>(hist + e);
+      int4 before = {0, 0, 0, 0}, total = {0, 0, 0, 0};
+#pragma unroll 16
+      for (int b = tid / width; b < nb; b += parts) {
+        const int4 n = rows[b * quads];
+        const int on = b < static_cast<int>(blockIdx.x) ? -1 : 0;
+        total.x += n.x; total.y += n.y; total.z += n.z; total.w += n.w;
+        before.x += n.x & on; before.y += n.y & on; before.z += n.z & on; before.w += n.w & on;
       }
-      atomicAdd(&all[e], total);
-      atomicAdd(&seen[e], before);
+      const int t[4] = {total.x, total.y, total.z, total.w}, f[4] = {before.x, before.y, before.z, before.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (e + i < E) {
+          atomicAdd(&all[e + i], t[i]);
+          atomicAdd(&seen[e + i], f[i]);
+        }
     }
     __syncthreads();
     offsets_of();
   }
   int bits = 0;
-  while ((1 << bits) <= E) ++bits;
-  const int64_t p0 = blockIdx.x * chunk, p1 = min(N, p0 + chunk);
+  while ((1 << bits) < E) ++bits;
   for (int64_t t0 = p0; t0 < p1; t0 += kTile) {
     const int n = static_cast<int>(min<int64_t>(kTile, p1 - t0));
     const int items = (n + kWg - 1) / kWg;    // pairs of a lane in this tile
@@ -126,37 +155,35 @@ __global__ __launch_bounds__(kWg) void k_dispatch_place(const int32_t* __restric
     const int w0 = wave * 64 * items + lane;
     int e[kItems], rank[kItems];
 #pragma unroll
-    for (int i = 0; i < kItems; ++i) {
-      const int at = w0 + 64 * i;
-      e[i] = E;
-      if (i < items && at < n) {
-        const int id = ids[t0 + at];
-        if (id >= 0 && id < E) e[i] = id;
-      }
-    }
+    for (int i = 0; i < kItems; ++i)
+      e[i] = i < items && w0 + 64 * i < n && id[i] >= 0 && id[i] < E ? id[i] : E;
+    if (t0 + kTile < p1) fetch(t0 + kTile);
 #pragma unroll
     for (int i = 0; i < kItems; ++i) {
       rank[i] = 0;
       if (i < items) {
-        unsigned long long same = ~0ull;
-        for (int b = 0; b < bits; ++b) {
-          const bool set = (e[i] >> b) & 1;
-          const unsigned long long v = __ballot(set);
-          same &= set ? v : ~v;
-        }
-        const int before = __popcll(same & ((1ull << lane) - 1));
         const bool on = e[i] < E;
+        const unsigned long long live = __ballot(on);
+        unsigned lo = static_cast<unsigned>(live), hi = static_cast<unsigned>(live >> 32);
+        for (int b = 0; b < bits; ++b) {
+          const unsigned set = -((static_cast<unsigned>(e[i]) >> b) & 1u);
+          const unsigned long long v = __ballot(set != 0);
+          lo &= ~(static_cast<unsigned>(v) ^ set);
+          hi &= ~(static_cast<unsigned>(v >> 32) ^ set);
+        }
+        const int before = __builtin_amdgcn_mbcnt_hi(hi, __builtin_amdgcn_mbcnt_lo(lo, 0));
         rank[i] = (on ? mine[e[i]] : 0) + before;
         // all lanes have read before the first of each expert writes; a wave's
         // LDS accesses stay in order
         __builtin_amdgcn_wave_barrier();
-        if (on && before == 0) mine[e[i]] = rank[i] + __popcll(same);
+        if (on && before == 0) mine[e[i]] = rank[i] + __popc(lo) + __popc(hi);
         __builtin_amdgcn_wave_barrier();
       }
     }
     __syncthreads();
+    int run = tid < E ? seen[tid] : 0;
+    const int prior = run;
     if (tid < E) {
-      int run = seen[tid];
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) {
         const int c = cnt[w * E + tid];
@@ -166,8 +193,14 @@ __global__ __launch_bounds__(kWg) void k_dispatch_place(const int32_t* __restric
       seen[tid] = run;
       if (ONE) all[tid] = run;
     }
-    __syncthreads();
-    if (ONE) offsets_of();
+    if (ONE) {
+      __syncthreads();
+      offsets_of();
+    } else {
+      const int at = scan_before(run - prior, wave_sum);
+      if (tid < E) slot0[tid] = at - prior;
+      __syncthreads();
+    }
 #pragma unroll
     for (int i = 0; i < kItems; ++i) {
       const int at = w0 + 64 * i;
@@ -176,9 +209,12 @@ __global__ __launch_bounds__(kWg) void k_dispatch_place(const int32_t* __restric
         int place = -1;
         if (e[i] < E) {
           const int r = mine[e[i]] + rank[i];
-          if (r < cap) {
-            place = start[e[i]] + r;
-            order[place] = static_cast<int32_t>(p);
+          if (r < cap) place = start[e[i]] + r;
+          if (ONE) {
+            if (place >= 0) order[place] = static_cast<int32_t>(p);
+          } else {
+            places[slot0[e[i]] + r] = place;
+            pairs[slot0[e[i]] + r] = static_cast<uint16_t>(at);
           }
         }
         position[p] = place;
@@ -186,6 +222,12 @@ __global__ __launch_bounds__(kWg) void k_dispatch_place(const int32_t* __restric
       }
     }
     __syncthreads();
+    if (!ONE) {
+      const int sorted = slot0[E - 1] + seen[E - 1];
+      for (int i = tid; i < sorted; i += kWg)
+        if (places[i] >= 0) order[places[i]] = static_cast<int32_t>(t0 + pairs[i]);
+      __syncthreads();
+    }
   }
 }
 
@@ -204,7 +246,7 @@ int64_t blocks_of(int64_t N) { return N <= kTile ? 1 : (N + chunk_of(N) - 1) / c
 
 }  // namespace
 
-int64_t dispatch_workspace(int64_t N, int E) { return N <= kTile ? 0 : 4 * blocks_of(N) * E; }
+int64_t dispatch_workspace(int64_t N, int E) { return N <= kTile ? 0 : 4 * blocks_of(N) * row_of(E); }
 
 hipError_t launch_dispatch(const int32_t* ids, int64_t N, int E, int64_t capacity, int32_t* load,
                            int32_t* offsets, int32_t* order, int32_t* position, void* ws,
@@ -218,7 +260,7 @@ hipError_t launch_dispatch(const int32_t* ids, int64_t N, int E, int64_t capacit
     int32_t* hist = static_cast<int32_t*>(ws);
     const unsigned grid = static_cast<unsigned>(blocks_of(N));
     k_dispatch_count<<<grid, kWg, 0, st>>>(ids, N, chunk_of(N), E, hist);
-    k_dispatch_place<false><<<grid, kWg, lds, st>>>(ids, N, chunk_of(N), E, capacity, hist, load, offsets, order, position);
+    k_dispatch_place<false><<<grid, kWg, lds + kTile * 6, st>>>(ids, N, chunk_of(N), E, capacity, hist, load, offsets, order, position);
   }
   return hipGetLastError();
 }
