@@ -560,7 +560,7 @@ bo_status bo_measure_peak(int32_t what, int64_t iters, double* rate, void* strea
  * logits   device [T][stride] of `type`, the first V of each row used;
  *          aligned to its type, stride >= V (any when T <= 1)
  * tokens   device int64 [T], or NULL: no row has a token
- * inv_temperature  finite, > 0
+ * inv_temperature  in (0, 1e30]
  * top      0..min(V, BO_MAX_ALTERNATIVES)
  * logprob, entropy device [T] out;  rank device int32 [T] out
  * stats    device [T][2] out (what the gradient takes)

@@ -226,7 +226,7 @@ __global__ __launch_bounds__(kWg) void k_logprobs(LogprobArgs a, int splits, int
 
     // what is left of the row past its whole vectors: an element to a lane
     const bool owns_rest = part == splits - 1 && tid < rest;
-    const int jr = nv * KV + tid;
+    const int64_t jr = (int64_t)nv * KV + tid;
     float lr = owns_rest ? El::load(x[jr]) : kNegInf;
     for (int vb = v0; vb < v1; vb += kWg * U) {
       if (vb + kWg * U > v1) {
@@ -537,7 +537,7 @@ __global__ __launch_bounds__(kWg) void k_logprobs_grad(LogprobGradArgs a, int sp
     // (the row's last share has what is left past the whole vectors)
     const bool last = part == splits - 1;
     if (id < v0 * KV || id >= (last ? V_ : v1 * KV) || empty) id = -1;
-    const int jr = nv * KV + tid;
+    const int64_t jr = (int64_t)nv * KV + tid;
     const float lr = last && tid < rest ? El::load(x[jr]) : 0.0f;
     const float xi = id >= 0 ? El::load(x[id]) : 0.0f;     // before the row may be overwritten
     __syncthreads();

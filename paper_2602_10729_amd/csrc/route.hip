@@ -109,12 +109,20 @@ __device__ __forceinline__ float row_reduce(float v, int lpt, F f) {
   if (lpt > 16) v = f(v, swap_lanes<16>(v));
   return v;
 }
-template <int K, int XOR>
-__device__ __forceinline__ void join_lists(double* a) {
-  double b[K];
+// Every lane of the row takes the K best of the row's lists (one copy of the
+// code for all distances: the kernel runs its code once, so its fetch counts).
+template <int K>
+__device__ __forceinline__ void join_lists(double* a, int lane, int lpt) {
+#pragma unroll 1
+  for (int x = 1; x < lpt; x <<= 1) {
+    const int from = (lane ^ x) << 2;
+    double b[K];
 #pragma unroll
-  for (int i = 0; i < K; ++i) b[i] = swap_lanes<XOR>(a[i]);
-  keep_best<K, K>(a, b);
+    for (int i = 0; i < K; ++i)
+      b[i] = __hiloint2double(__builtin_amdgcn_ds_bpermute(from, __double2hiint(a[i])),
+                              __builtin_amdgcn_ds_bpermute(from, __double2loint(a[i])));
+    keep_best<K, K>(a, b);
+  }
 }
 
 // A lane's `span` elements of a row of E from `first` on, -inf past the end.
@@ -229,9 +237,9 @@ __global__ __launch_bounds__(kWg, K <= 8 && GROUPS != kAnyGroups ? 4 : 1) void k
       return __builtin_amdgcn_exp2f((t - m) * kLog2e) * inv;
     };
     // what is compared, eight experts at a time; -inf where one cannot be chosen
-    const auto values = [&](int b, float (&v)[8]) {
+    const auto values = [&](int at, int b, float (&v)[8]) {      // (block b, held at place `at`)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = logit(8 * b + e);
+      for (int e = 0; e < 8; ++e) v[e] = logit(8 * at + e);
       if (scored) {
         if (a.score == BO_SCORE_SIGMOID) {
 #pragma unroll
@@ -248,7 +256,7 @@ __global__ __launch_bounds__(kWg, K <= 8 && GROUPS != kAnyGroups ? 4 : 1) void k
           v[4] += hi.x; v[5] += hi.y; v[6] += hi.z; v[7] += hi.w;
         }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = logit(8 * b + e) > kNegInf ? v[e] : kNegInf;
+        for (int e = 0; e < 8; ++e) v[e] = logit(8 * at + e) > kNegInf ? v[e] : kNegInf;
       }
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = fmaxf(v[e], kNegInf);     // a NaN is no choice
@@ -272,7 +280,7 @@ __global__ __launch_bounds__(kWg, K <= 8 && GROUPS != kAnyGroups ? 4 : 1) void k
       for (int b = 0; b < kBlocks; ++b)
         if (8 * b < span) {
           float v[8];
-          values(b, v);
+          values(b, b, v);
           float b1 = kNegInf, b2 = kNegInf;
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
@@ -310,7 +318,7 @@ __global__ __launch_bounds__(kWg, K <= 8 && GROUPS != kAnyGroups ? 4 : 1) void k
       for (int b = 0; b < kBlocks; ++b)
         if (8 * b < span) {
           float v[8];
-          values(b, v);
+          values(b, b, v);
 #pragma unroll
           for (int e = 0; e < 8; ++e) val[at_of(first + 8 * b) + e] = v[e];
         }
@@ -326,40 +334,40 @@ __global__ __launch_bounds__(kWg, K <= 8 && GROUPS != kAnyGroups ? 4 : 1) void k
           for (int e = g * per; e < (g + 1) * per; ++e) val[at_of(e)] = kNegInf;
       __syncthreads();
     }
-    // the lane's best
+    // the lane's best, eight experts at a time in one copy of the code: what comes
+    // next moves to the front
     double best[K];
     constexpr int B = K < 8 ? K : 8;
 #pragma unroll
     for (int i = 0; i < K; ++i) best[i] = 0.0;
+#pragma unroll 1
+    for (int b = 0; 8 * b < span; ++b) {
+      float v[8];
+      if constexpr (GROUPS == kBlockGroups) {
 #pragma unroll
-    for (int b = 0; b < kBlocks; ++b) {
-      if (8 * b < span) {
-        float v[8];
-        if constexpr (GROUPS == kBlockGroups) {
+        for (int e = 0; e < 8; ++e) v[e] = kept[e];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = kept[8 * b + e];
-        } else if constexpr (GROUPS == kAnyGroups) {
+        for (int i = 0; i < kSpan - 8; ++i) kept[i] = kept[i + 8];
+      } else {
+        if constexpr (GROUPS == kAnyGroups) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
             v[e] = val[at_of(first + 8 * b) + e];
-            if (!a.bias) v[e] = v[e] > kNegInf ? logit(8 * b + e) : kNegInf;
+            if (!a.bias) v[e] = v[e] > kNegInf ? logit(e) : kNegInf;
           }
         } else {
-          values(b, v);
+          values(0, b, v);
         }
 #pragma unroll
-        for (int p = 0; p < 8 / B; ++p) {
-          double key[B];
+        for (int p = 0; p < (kSpan - 8) / V::kVec; ++p) q[p] = q[p + 8 / V::kVec];
+      }
 #pragma unroll
-          for (int e = 0; e < B; ++e) key[e] = make_key(v[p * B + e], 8 * b + p * B + e);
-          sort<B>(key);
-          if (b == 0 && p == 0) {
+      for (int p = 0; p < 8 / B; ++p) {
+        double key[B];
 #pragma unroll
-            for (int e = 0; e < B; ++e) best[e] = key[e];
-          } else {
-            keep_best<K, B>(best, key);
-          }
-        }
+        for (int e = 0; e < B; ++e) key[e] = make_key(v[p * B + e], 8 * b + p * B + e);
+        sort<B>(key);
+        keep_best<K, B>(best, key);
       }
     }
     // the row's best: the lane joins the key
@@ -367,11 +375,7 @@ __global__ __launch_bounds__(kWg, K <= 8 && GROUPS != kAnyGroups ? 4 : 1) void k
     for (int i = 0; i < K; ++i)
       best[i] = __hiloint2double(__double2hiint(best[i]),
                                  __double2loint(best[i]) | ((31 - sub) << 5));
-    if (lpt > 1) join_lists<K, 1>(best);
-    if (lpt > 2) join_lists<K, 2>(best);
-    if (lpt > 4) join_lists<K, 4>(best);
-    if (lpt > 8) join_lists<K, 8>(best);
-    if (lpt > 16) join_lists<K, 16>(best);
+    join_lists<K>(best, lane, lpt);
     if constexpr (GROUPS == kAnyGroups) __syncthreads();
     // weights: lane `sub` takes choices sub, sub + lpt, ..
     int* cid = reinterpret_cast<int*>(lds[wave]) + slot * K;

@@ -79,8 +79,8 @@ bo_status check_logprob_sizes(int32_t type, int64_t T, int64_t V, float it, int3
   const std::string W(where);
   if (bad_type(type)) return fail(BO_ERR_INVALID_ARGUMENT, W + ": unknown type");
   if (T < 0 || V < 1) return fail(BO_ERR_INVALID_ARGUMENT, W + ": T < 0 or V < 1");
-  if (!(it > 0.0f) || !std::isfinite(it))
-    return fail(BO_ERR_INVALID_ARGUMENT, W + ": inv_temperature must be finite and > 0");
+  if (!(it > 0.0f) || !(it <= 1e30f))     // (beyond, a product with log2(e) or a logit is no number)
+    return fail(BO_ERR_INVALID_ARGUMENT, W + ": inv_temperature must be in (0, 1e30]");
   if (top < 0) return fail(BO_ERR_INVALID_ARGUMENT, W + ": top < 0");
   if (V >= ((int64_t)1 << 31) || T > kMaxRows) return fail(BO_ERR_CAPACITY, W + ": T or V beyond limit");
   if (top > BO_MAX_ALTERNATIVES) return fail(BO_ERR_CAPACITY, W + ": top beyond BO_MAX_ALTERNATIVES");

@@ -154,6 +154,29 @@ def test_logprobs_masks(V, kind):
     assert not r.logprob.any() and not r.rank.any()
 
 
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+def test_signalling_nans_hide_nothing(kind):
+    """NaNs of every kind among the logits: never alternatives, never counted, and
+    they cost no other logit its place."""
+    import torch
+    import paper_2602_10729_amd as bo
+    _announce("logprobs NaN kinds", kind)
+    rng = np.random.default_rng(21)
+    bits = {"f32": (torch.int32, [0x7F800001, 0x7FC00000, -0x7FFFFF, -1]),
+            "bf16": (torch.int16, [0x7F81, 0x7FC0, -0x7F, -1]),
+            "f16": (torch.int16, [0x7C01, 0x7E00, -0x3FF, -1])}[kind]
+    x = _logits(rng, 4, 9000, kind)
+    for r in range(4):
+        at = torch.from_numpy(rng.choice(9000, 900, replace=False)).cuda()
+        x[r].view(bits[0])[at] = bits[1][r]
+    tok = np.array([5, 6, 7, 8])
+    r = bo.token_logprobs(x, _tokens(tok), top=16)
+    o = R.token_logprobs(_np(x), tok, 16)
+    assert np.array_equal(r.top_ids.cpu().numpy(), o["top_ids"])
+    assert np.array_equal(r.rank.cpu().numpy(), o["rank"])
+    assert bool(r.entropy.isnan().all()) and bool(r.logprob.isnan().all())
+
+
 def test_logprobs_far_from_zero():
     """Rows whose logits all lie far from 0, and rows whose largest comes late."""
     import paper_2602_10729_amd as bo

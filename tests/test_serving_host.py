@@ -26,6 +26,7 @@ def _lp(L, type=0, T=2, V=10, stride=10, it=1.0, top=2, logits=P, ws=P, wb=1 << 
 def test_logprob_refusals(L):
     assert _lp(L, type=3) == INVALID and _lp(L, T=-1) == INVALID and _lp(L, V=0) == INVALID
     assert _lp(L, it=0.0) == INVALID and _lp(L, it=float("inf")) == INVALID
+    assert _lp(L, it=1.1e30) == INVALID
     assert _lp(L, it=float("nan")) == INVALID and _lp(L, top=-1) == INVALID
     assert _lp(L, top=11) == INVALID and _lp(L, V=100, stride=100, top=65) == CAPACITY
     assert _lp(L, V=2 ** 31, stride=2 ** 31) == CAPACITY and _lp(L, T=2 ** 62) == CAPACITY
