@@ -91,7 +91,7 @@ __device__ __forceinline__ void keep_best(double* a, const double* b) {
 __device__ __forceinline__ double make_key(float v, int place) {
   const unsigned o = code_of(v);
   return __hiloint2double(static_cast<int>(kExpTwo52 | (o >> 12)),
-                          static_cast<int>((o << 20) | static_cast<unsigned>(kSpan - 1 - place)));
+                          static_cast<int>((o << 20) | static_cast<unsigned>(31 - place)));
 }
 
 // (the code of -inf is 0x007FFFFF, the next one 0x00800000)
@@ -125,29 +125,24 @@ __device__ __forceinline__ void join_lists(double* a, int lane, int lpt) {
   }
 }
 
-// A lane's `span` elements of a row of E from `first` on, -inf past the end.
+// A lane's SPAN elements of a row of E from `first` on, -inf past the end.
 // Every lane loads (a load that only some lanes make waits for the one before
 // it): what would reach past the row starts earlier and is moved up.
-template <int TYPE>
-__device__ __forceinline__ void load_span(Vec<TYPE> (&q)[kSpan / Vec<TYPE>::kVec],
-                                          const typename Elem<TYPE>::T* x, int first, int span, int E) {
+template <int TYPE, int SPAN>
+__device__ __forceinline__ void load_span(Vec<TYPE> (&q)[SPAN / Vec<TYPE>::kVec],
+                                          const typename Elem<TYPE>::T* x, int first, int E) {
   constexpr int KV = Vec<TYPE>::kVec;
   if (E >= KV) {
 #pragma unroll
-    for (int p = 0; p < kSpan / KV; ++p)
-      if (p * KV < span) q[p].load(x + min(first + p * KV, E - KV));
+    for (int p = 0; p < SPAN / KV; ++p) q[p].load(x + min(first + p * KV, E - KV));
 #pragma unroll
-    for (int p = 0; p < kSpan / KV; ++p) {
-      if (p * KV < span) {
-        const int past = first + p * KV - (E - KV);
-        if (__any(past > 0)) q[p].drop(max(past, 0));
-      } else {
-        q[p].fill_masked();
-      }
+    for (int p = 0; p < SPAN / KV; ++p) {
+      const int past = first + p * KV - (E - KV);
+      if (__any(past > 0)) q[p].drop(max(past, 0));
     }
   } else {
 #pragma unroll
-    for (int p = 0; p < kSpan / KV; ++p) q[p].fill_masked();
+    for (int p = 0; p < SPAN / KV; ++p) q[p].fill_masked();
     if (first == 0) q[0].load_part(x, E);
   }
 }
@@ -168,29 +163,27 @@ __device__ __forceinline__ void top_two(float& b1, float& b2, float o1, float o2
 // How the groups lie: none (or none dropped), each of whole eights, or anyhow.
 enum { kNoGroups, kBlockGroups, kAnyGroups };
 
-// 1 << shift lanes a row. `div` is 65536 / eights per group, rounded up
+// 1 << shift lanes a row, NB eights of experts each. `div` is 65536 / eights per group, rounded up
 // (kBlockGroups): eight / (eights per group) = eight * div >> 16 for up to 128.
-template <int TYPE, int K, int GROUPS>
+template <int TYPE, int K, int GROUPS, int NB>
 __global__ __launch_bounds__(kWg, K <= 8 && GROUPS != kAnyGroups ? 4 : 1) void k_route(RouteArgs a, int shift, int div) {
   using El = Elem<TYPE>;
   using V = Vec<TYPE>;
-  constexpr int kBlocks = kSpan / 8;
+  constexpr int SPAN = 8 * NB;
   // per wave: choices and what they weigh, and before them the groups' work
   constexpr int kChoice = 2 * 64 * K;
-  constexpr int kGroup = GROUPS == kNoGroups ? 0 : GROUPS == kBlockGroups ? 64 * kBlocks * 3 + 64 * kBlocks
-                                                                         : 64 * (kSpan + 1) + 64 * kSpan / 2;
+  constexpr int kGroup = GROUPS == kNoGroups ? 0 : GROUPS == kBlockGroups ? 64 * NB * 4
+                                                                         : 64 * (SPAN + 1) + 64 * SPAN / 2;
   __shared__ float lds[kWg / 64][kChoice > kGroup ? kChoice : kGroup];
   __shared__ alignas(16) float lds_bias[BO_MAX_EXPERTS + 8 * kSpan];
   const auto fmax2 = [](float p, float q) { return fmaxf(p, q); };
   const auto fadd2 = [](float p, float q) { return p + q; };
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lpt = 1 << shift, sub = lane & (lpt - 1), slot = lane >> shift, rows = 64 >> shift;
-  // experts a lane holds: whole eights, consecutive ones
-  const int span = ((((a.E + 7) >> 3) + lpt - 1) >> shift) << 3;
-  const int first = sub * span;
+  const int first = sub * SPAN;
   const bool scored = GROUPS != kNoGroups || a.bias;      // else the logits are compared
   if (a.bias) {
-    for (int j = threadIdx.x; j < span * lpt; j += kWg) lds_bias[j] = j < a.E ? a.bias[j] : kNegInf;
+    for (int j = threadIdx.x; j < SPAN * lpt; j += kWg) lds_bias[j] = j < a.E ? a.bias[j] : kNegInf;
     __syncthreads();
   }
   const int64_t step = (int64_t)gridDim.x * (kWg / 64) * rows;
@@ -199,8 +192,8 @@ __global__ __launch_bounds__(kWg, K <= 8 && GROUPS != kAnyGroups ? 4 : 1) void k
     const bool live = row < a.T;
     const typename El::T* x =
         static_cast<const typename El::T*>(a.logits) + (live ? row : 0) * a.stride;
-    V q[kSpan / V::kVec];
-    load_span<TYPE>(q, x, first, span, a.E);
+    V q[SPAN / V::kVec];
+    load_span<TYPE, SPAN>(q, x, first, a.E);
     const auto logit = [&](int i) { return q[i / V::kVec].get(i % V::kVec); };
     // softmax statistics; a row with a NaN or +inf has no choice
     float m = 0.0f, inv = 1.0f;
@@ -208,14 +201,10 @@ __global__ __launch_bounds__(kWg, K <= 8 && GROUPS != kAnyGroups ? 4 : 1) void k
     if (a.score == BO_SCORE_SOFTMAX) {
       m = kNegInf;
 #pragma unroll
-      for (int b = 0; b < kBlocks; ++b)
-        if (8 * b < span) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            m = max2(m, logit(8 * b + e));
-            bad = bad || __builtin_isnan(logit(8 * b + e));
-          }
-        }
+      for (int i = 0; i < SPAN; ++i) {
+        m = max2(m, logit(i));
+        bad = bad || __builtin_isnan(logit(i));
+      }
       m = row_reduce(m, lpt, fmax2);
       bad = bad || m == __builtin_huge_valf();
       bad = (__ballot(bad) >> (slot << shift) & (~0ull >> (64 - lpt))) != 0;
@@ -223,11 +212,7 @@ __global__ __launch_bounds__(kWg, K <= 8 && GROUPS != kAnyGroups ? 4 : 1) void k
       if (scored || !a.renorm) {
         float t = 0.0f;
 #pragma unroll
-        for (int b = 0; b < kBlocks; ++b)
-          if (8 * b < span) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) t += __builtin_amdgcn_exp2f((logit(8 * b + e) - m) * kLog2e);
-          }
+        for (int i = 0; i < SPAN; ++i) t += __builtin_amdgcn_exp2f((logit(i) - m) * kLog2e);
         inv = 1.0f / row_reduce(t, lpt, fadd2);
       }
     }
@@ -261,8 +246,8 @@ __global__ __launch_bounds__(kWg, K <= 8 && GROUPS != kAnyGroups ? 4 : 1) void k
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = fmaxf(v[e], kNegInf);     // a NaN is no choice
     };
-    float kept[GROUPS == kBlockGroups ? kSpan : 1];
-    float* val = lds[wave] + slot * lpt * (kSpan + 1);
+    float kept[GROUPS == kBlockGroups ? SPAN : 1];
+    float* val = lds[wave] + slot * lpt * (SPAN + 1);
     // a group that top_groups or more come before is dropped
     const auto dropped = [&](const unsigned* grp, int g) {
       const unsigned mine = grp[g];
@@ -272,13 +257,12 @@ __global__ __launch_bounds__(kWg, K <= 8 && GROUPS != kAnyGroups ? 4 : 1) void k
     };
     if constexpr (GROUPS == kBlockGroups) {
       // the best two of each eight, then of each group
-      float2* two = reinterpret_cast<float2*>(lds[wave]) + slot * lpt * kBlocks;
-      unsigned* grp = reinterpret_cast<unsigned*>(lds[wave] + 64 * kBlocks * 2) + slot * lpt * kBlocks;
-      unsigned* drop = grp + 64 * kBlocks;
+      float2* two = reinterpret_cast<float2*>(lds[wave]) + slot * lpt * NB;
+      unsigned* grp = reinterpret_cast<unsigned*>(lds[wave] + 64 * NB * 2) + slot * lpt * NB;
+      unsigned* drop = grp + 64 * NB;
       const int eights = a.E / a.groups / 8, at = first >> 3;
 #pragma unroll
-      for (int b = 0; b < kBlocks; ++b)
-        if (8 * b < span) {
+      for (int b = 0; b < NB; ++b) {
           float v[8];
           values(b, b, v);
           float b1 = kNegInf, b2 = kNegInf;
@@ -300,8 +284,7 @@ __global__ __launch_bounds__(kWg, K <= 8 && GROUPS != kAnyGroups ? 4 : 1) void k
       for (int g = sub; g < a.groups; g += lpt) drop[g] = dropped(grp, g);
       __syncthreads();
 #pragma unroll
-      for (int b = 0; b < kBlocks; ++b)
-        if (8 * b < span) {
+      for (int b = 0; b < NB; ++b) {
           const bool out = drop[min((at + b) * div >> 16, a.groups - 1)];
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
@@ -313,10 +296,9 @@ __global__ __launch_bounds__(kWg, K <= 8 && GROUPS != kAnyGroups ? 4 : 1) void k
     }
     if constexpr (GROUPS == kAnyGroups) {
       const int per = a.E / a.groups;
-      unsigned* grp = reinterpret_cast<unsigned*>(lds[wave] + 64 * (kSpan + 1)) + slot * lpt * (kSpan / 2);
+      unsigned* grp = reinterpret_cast<unsigned*>(lds[wave] + 64 * (SPAN + 1)) + slot * lpt * (SPAN / 2);
 #pragma unroll
-      for (int b = 0; b < kBlocks; ++b)
-        if (8 * b < span) {
+      for (int b = 0; b < NB; ++b) {
           float v[8];
           values(b, b, v);
 #pragma unroll
@@ -341,13 +323,13 @@ __global__ __launch_bounds__(kWg, K <= 8 && GROUPS != kAnyGroups ? 4 : 1) void k
 #pragma unroll
     for (int i = 0; i < K; ++i) best[i] = 0.0;
 #pragma unroll 1
-    for (int b = 0; 8 * b < span; ++b) {
+    for (int b = 0; b < NB; ++b) {
       float v[8];
       if constexpr (GROUPS == kBlockGroups) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = kept[e];
 #pragma unroll
-        for (int i = 0; i < kSpan - 8; ++i) kept[i] = kept[i + 8];
+        for (int i = 0; i < SPAN - 8; ++i) kept[i] = kept[i + 8];
       } else {
         if constexpr (GROUPS == kAnyGroups) {
 #pragma unroll
@@ -359,7 +341,7 @@ __global__ __launch_bounds__(kWg, K <= 8 && GROUPS != kAnyGroups ? 4 : 1) void k
           values(0, b, v);
         }
 #pragma unroll
-        for (int p = 0; p < (kSpan - 8) / V::kVec; ++p) q[p] = q[p + 8 / V::kVec];
+        for (int p = 0; p < (SPAN - 8) / V::kVec; ++p) q[p] = q[p + 8 / V::kVec];
       }
 #pragma unroll
       for (int p = 0; p < 8 / B; ++p) {
@@ -384,7 +366,7 @@ __global__ __launch_bounds__(kWg, K <= 8 && GROUPS != kAnyGroups ? 4 : 1) void k
 #pragma unroll
       for (int i = 0; i < K; ++i) {
         const int lo = __double2loint(best[i]);
-        cid[i] = is_choice(best[i]) && !bad ? (31 - ((lo >> 5) & 31)) * span + (kSpan - 1 - (lo & 31)) : -1;
+        cid[i] = is_choice(best[i]) && !bad ? (31 - ((lo >> 5) & 31)) * SPAN + (31 - (lo & 31)) : -1;
       }
     }
     __syncthreads();
@@ -426,78 +408,63 @@ __global__ __launch_bounds__(kWg, K <= 8 && GROUPS != kAnyGroups ? 4 : 1) void k
 
 // The same lanes hold a row: each choice's term goes to its expert's place in
 // LDS, then every lane adds the dense part (softmax, not renormalised: -scale
-// s_j sum_k s_k g_k) to its experts' and writes them. K >= top choices, of
-// which a lane takes sub, sub + lpt, ..
-template <int TYPE, int K>
+// s_j sum_k s_k g_k) to its experts' and writes them. A lane takes choices sub,
+// sub + lpt, .., C at most.
+template <int TYPE, int C, int NB>
 __global__ __launch_bounds__(kWg) void k_route_grad(RouteGradArgs a, int shift) {
   using El = Elem<TYPE>;
   using V = Vec<TYPE>;
-  constexpr int kParts = kSpan / V::kVec;
+  constexpr int SPAN = 8 * NB, kParts = SPAN / V::kVec;
   extern __shared__ float lds_term[];       // [waves][rows][row_words]
   const auto fmax2 = [](float p, float q) { return fmaxf(p, q); };
   const auto fadd2 = [](float p, float q) { return p + q; };
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lpt = 1 << shift, sub = lane & (lpt - 1), slot = lane >> shift, rows = 64 >> shift;
-  const int span = ((((a.E + 7) >> 3) + lpt - 1) >> shift) << 3;
-  const int first = sub * span;
+  const int first = sub * SPAN;
   const int64_t step = (int64_t)gridDim.x * (kWg / 64) * rows;
   const bool softmax = a.score == BO_SCORE_SOFTMAX, dense = softmax && !a.renorm;
-  float* term = lds_term + (wave * rows + slot) * row_words(span << shift);
+  float* term = lds_term + (wave * rows + slot) * row_words(SPAN << shift);
   for (int64_t base = (int64_t)blockIdx.x * (kWg / 64) * rows; base < a.T; base += step) {
     const int64_t row = base + wave * rows + slot;
     const bool live = row < a.T;
     const int64_t r = live ? row : 0;
     const typename El::T* x = static_cast<const typename El::T*>(a.logits) + r * a.stride;
     // a lane's choices: expert, logit, the weight's gradient
-    int id[K];
-    float l[K], g[K];
+    int id[C];
+    float l[C], g[C];
 #pragma unroll
-    for (int t = 0; t < K; ++t)
-      if (t * lpt < a.top) {
-        const int n = min(t * lpt + sub, a.top - 1);
-        id[t] = a.ids[r * a.top + n];
-        g[t] = a.g[r * a.top + n];
-        if (id[t] >= a.E || t * lpt + sub >= a.top) id[t] = -1;
-      }
+    for (int t = 0; t < C; ++t) {
+      const int n = min(t * lpt + sub, a.top - 1);
+      id[t] = a.ids[r * a.top + n];
+      g[t] = a.g[r * a.top + n];
+      if (id[t] >= a.E || t * lpt + sub >= a.top) id[t] = -1;
+    }
 #pragma unroll
-    for (int t = 0; t < K; ++t)
-      if (t * lpt < a.top) l[t] = El::load(x[max(id[t], 0)]);
+    for (int t = 0; t < C; ++t) l[t] = El::load(x[max(id[t], 0)]);
     V q[kParts];
     float m = 0.0f, inv = 1.0f;
     if (dense) {
-      load_span<TYPE>(q, x, first, span, a.E);
+      load_span<TYPE, SPAN>(q, x, first, a.E);
       m = kNegInf;
 #pragma unroll
-      for (int p = 0; p < kParts; ++p)
-        if (p * V::kVec < span) {
-#pragma unroll
-          for (int e = 0; e < V::kVec; ++e) m = max2(m, q[p].get(e));
-        }
+      for (int i = 0; i < SPAN; ++i) m = max2(m, q[i / V::kVec].get(i % V::kVec));
       m = row_reduce(m, lpt, fmax2);
       m = m == kNegInf ? 0.0f : m;
       float t = 0.0f;
 #pragma unroll
-      for (int p = 0; p < kParts; ++p)
-        if (p * V::kVec < span) {
-#pragma unroll
-          for (int e = 0; e < V::kVec; ++e) t += __builtin_amdgcn_exp2f((q[p].get(e) - m) * kLog2e);
-        }
+      for (int i = 0; i < SPAN; ++i)
+        t += __builtin_amdgcn_exp2f((q[i / V::kVec].get(i % V::kVec) - m) * kLog2e);
       inv = 1.0f / row_reduce(t, lpt, fadd2);
     }
 #pragma unroll
-    for (int b = 0; b < kSpan / 8; ++b)
-      if (8 * b < span) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) term[at_of(first + 8 * b) + e] = 0.0f;
-      }
+    for (int i = 0; i < SPAN; ++i) term[at_of(first) + i] = 0.0f;
     const auto sigm = [](float t) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-t * kLog2e)); };
     float hi = kNegInf, any = 0.0f;
 #pragma unroll
-    for (int t = 0; t < K; ++t)
-      if (t * lpt < a.top) {
-        hi = id[t] >= 0 ? fmaxf(hi, l[t]) : hi;
-        any = id[t] >= 0 ? 1.0f : any;
-      }
+    for (int t = 0; t < C; ++t) {
+      hi = id[t] >= 0 ? fmaxf(hi, l[t]) : hi;
+      any = id[t] >= 0 ? 1.0f : any;
+    }
     if (a.renorm) {
       hi = row_reduce(hi, lpt, fmax2);
       if (!softmax) hi = fminf(hi, 0.0f);
@@ -511,21 +478,20 @@ __global__ __launch_bounds__(kWg) void k_route_grad(RouteGradArgs a, int shift) 
       const float w = __builtin_amdgcn_exp2f((t - hi) * kLog2e);
       return softmax ? w : w * sigm(-t);
     };
-    float total = 0.0f, wg = 0.0f, w[K];
+    float total = 0.0f, wg = 0.0f, w[C];
 #pragma unroll
-    for (int t = 0; t < K; ++t)
-      if (t * lpt < a.top) {
-        w[t] = id[t] >= 0 ? weight(l[t]) : 0.0f;
-        total += w[t];
-        if (id[t] >= 0) wg = fmaf(w[t], g[t], wg);
-      }
+    for (int t = 0; t < C; ++t) {
+      w[t] = id[t] >= 0 ? weight(l[t]) : 0.0f;
+      total += w[t];
+      wg = id[t] >= 0 ? fmaf(w[t], g[t], wg) : wg;
+    }
     if (a.renorm) total = row_reduce(total, lpt, fadd2);
     if (a.renorm || dense) wg = row_reduce(wg, lpt, fadd2);
     const float norm = a.renorm ? 1.0f / total : 1.0f, mean = a.renorm ? wg * norm : 0.0f;
     __syncthreads();
 #pragma unroll
-    for (int t = 0; t < K; ++t)
-      if (t * lpt < a.top && id[t] >= 0) {
+    for (int t = 0; t < C; ++t)
+      if (id[t] >= 0) {
         const float d = a.scale * (w[t] * norm) * (g[t] - mean);
         term[at_of(id[t])] = softmax ? d : d * sigm(-l[t]);
       }
@@ -535,21 +501,19 @@ __global__ __launch_bounds__(kWg) void k_route_grad(RouteGradArgs a, int shift) 
 #pragma unroll
     for (int p = 0; p < kParts; ++p) {
       const int j = first + p * V::kVec;
-      if (p * V::kVec < span) {
-        float v[V::kVec];
+      float v[V::kVec];
 #pragma unroll
-        for (int e = 0; e < V::kVec; ++e) v[e] = term[at_of(j) + e];
-        if (dense) {
+      for (int e = 0; e < V::kVec; ++e) v[e] = term[at_of(first) + p * V::kVec + e];
+      if (dense) {
 #pragma unroll
-          for (int e = 0; e < V::kVec; ++e) {
-            const float s = __builtin_amdgcn_exp2f((q[p].get(e) - m) * kLog2e);
-            v[e] = back != 0.0f ? fmaf(back, s, v[e]) : v[e];
-          }
+        for (int e = 0; e < V::kVec; ++e) {
+          const float s = __builtin_amdgcn_exp2f((q[p].get(e) - m) * kLog2e);
+          v[e] = back != 0.0f ? fmaf(back, s, v[e]) : v[e];
         }
-        q[p].set_all(v);
-        if (live && j + V::kVec <= a.E) q[p].store(out + j);
-        else if (live && j < a.E) q[p].store_part(out + j, a.E - j);
       }
+      q[p].set_all(v);
+      if (live && j + V::kVec <= a.E) q[p].store(out + j);
+      else if (live && j < a.E) q[p].store_part(out + j, a.E - j);
     }
     __syncthreads();
   }
@@ -568,40 +532,51 @@ unsigned row_blocks(int64_t T, int shift) {
   return static_cast<unsigned>(std::min<int64_t>((T + rows - 1) / rows, 1 << 20));
 }
 
-// What fits the smallest list of at least `top`.
+// The smallest of 1, 2, 4, 8, 16, 32 that is at least n, as a constant.
 template <typename F>
-void by_top(int top, F f) {
-  if (top <= 2) f(std::integral_constant<int, 2>());
-  else if (top <= 4) f(std::integral_constant<int, 4>());
-  else if (top <= 8) f(std::integral_constant<int, 8>());
-  else if (top <= 16) f(std::integral_constant<int, 16>());
+void by_size(int n, F f) {
+  if (n <= 1) f(std::integral_constant<int, 1>());
+  else if (n <= 2) f(std::integral_constant<int, 2>());
+  else if (n <= 4) f(std::integral_constant<int, 4>());
+  else if (n <= 8) f(std::integral_constant<int, 8>());
+  else if (n <= 16) f(std::integral_constant<int, 16>());
   else f(std::integral_constant<int, 32>());
 }
+// Eights of experts that a lane holds (1, 2 or 4).
+int eights_of(int E, int shift) { return (((E + 7) >> 3) + (1 << shift) - 1) >> shift; }
 
 template <int TYPE>
 hipError_t launch_typed(const RouteArgs& a, hipStream_t st) {
   const int shift = lanes_shift(a.T, a.E);
   const unsigned grid = row_blocks(a.T, shift);
-  const int per = a.E / a.groups, eights = per / 8;
-  by_top(a.top, [&](auto k) {
-    constexpr int K = decltype(k)::value;
-    if (a.groups == 1 || a.top_groups == a.groups)
-      k_route<TYPE, K, kNoGroups><<<grid, kWg, 0, st>>>(a, shift, 0);
-    else if (per % 8 == 0)
-      k_route<TYPE, K, kBlockGroups><<<grid, kWg, 0, st>>>(a, shift, (65536 + eights - 1) / eights);
-    else
-      k_route<TYPE, K, kAnyGroups><<<grid, kWg, 0, st>>>(a, shift, 0);
+  const int per = a.E / a.groups, eights = per / 8, div = eights ? (65536 + eights - 1) / eights : 0;
+  const bool grouped = a.groups > 1 && a.top_groups < a.groups;
+  by_size(a.top, [&](auto k) {
+    by_size(eights_of(a.E, shift), [&](auto nb) {
+      // (one code for lists of one and two; groups of any size, and long lists,
+      // are rare: they take the widest lanes)
+      constexpr int K = decltype(k)::value < 2 ? 2 : decltype(k)::value;
+      constexpr int NB = K > 8 || decltype(nb)::value > 4 ? 4 : decltype(nb)::value;
+      if (!grouped) k_route<TYPE, K, kNoGroups, NB><<<grid, kWg, 0, st>>>(a, shift, 0);
+      else if (per % 8 == 0) k_route<TYPE, K, kBlockGroups, NB><<<grid, kWg, 0, st>>>(a, shift, div);
+      else k_route<TYPE, K, kAnyGroups, 4><<<grid, kWg, 0, st>>>(a, shift, 0);
+    });
   });
   return hipGetLastError();
 }
 
 template <int TYPE>
 hipError_t launch_typed(const RouteGradArgs& a, hipStream_t st) {
-  const int shift = lanes_shift(a.T, a.E);
+  const int shift = lanes_shift(a.T, a.E), lpt = 1 << shift;
   const unsigned grid = row_blocks(a.T, shift);
-  const int span = ((((a.E + 7) >> 3) + (1 << shift) - 1) >> shift) << 3;
-  const size_t lds = sizeof(float) * (kWg >> shift) * row_words(span << shift);
-  by_top(a.top, [&](auto k) { k_route_grad<TYPE, decltype(k)::value><<<grid, kWg, lds, st>>>(a, shift); });
+  by_size((a.top + lpt - 1) / lpt, [&](auto c) {
+    by_size(eights_of(a.E, shift), [&](auto nb) {
+      constexpr int C = decltype(c)::value;
+      constexpr int NB = C > 8 || decltype(nb)::value > 4 ? 4 : decltype(nb)::value;
+      const size_t lds = sizeof(float) * (kWg >> shift) * row_words((8 * NB) << shift);
+      k_route_grad<TYPE, C, NB><<<grid, kWg, lds, st>>>(a, shift);
+    });
+  });
   return hipGetLastError();
 }
 
