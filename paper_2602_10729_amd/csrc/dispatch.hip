@@ -14,6 +14,7 @@
 // What fits one tile takes one launch. Nothing depends on the order in which
 // atomics arrive: they only add integers.
 #include <algorithm>
+#include <type_traits>
 
 #include "serving.h"
 
@@ -22,8 +23,7 @@ namespace {
 
 constexpr int kWg = 1024;
 constexpr int kWaves = kWg / 64;
-constexpr int kItems = 8;                 // pairs a lane holds
-constexpr int kTile = kWg * kItems;
+constexpr int kMaxItems = 8;              // pairs a lane holds, at most
 constexpr int kMaxBlocks = 256;
 
 // Words of a block's counts: whole 16-byte groups.
@@ -65,7 +65,8 @@ __device__ int scan_before(int kept, int* wave_sum) {
 
 // Dynamic LDS: the waves' counts [kWaves][E]; unless ONE, the tile's places in
 // `order` and pairs, sorted by expert.
-template <bool ONE>
+// ITEMS: pairs a lane holds; a tile is kWg times as many.
+template <bool ONE, int ITEMS>
 __global__ __launch_bounds__(kWg) void k_dispatch_place(const int32_t* __restrict__ ids, int64_t N,
                                                         int64_t chunk, int E, int64_t capacity,
                                                         const int32_t* __restrict__ hist,
@@ -73,6 +74,7 @@ __global__ __launch_bounds__(kWg) void k_dispatch_place(const int32_t* __restric
                                                         int32_t* __restrict__ offsets,
                                                         int32_t* __restrict__ order,
                                                         int32_t* __restrict__ position) {
+  constexpr int kTile = kWg * ITEMS;
   extern __shared__ int32_t cnt[];
   int32_t* places = cnt + kWaves * E;
   uint16_t* pairs = reinterpret_cast<uint16_t*>(places + kTile);
@@ -108,12 +110,12 @@ __global__ __launch_bounds__(kWg) void k_dispatch_place(const int32_t* __restric
   // a tile: wave after wave, 64 pairs at a time (past its end the last pair
   // again); the first is on its way while the counts are summed
   const int64_t p0 = blockIdx.x * chunk, p1 = min(N, p0 + chunk);
-  int id[kItems];
+  const int w0 = wave * 64 * ITEMS + lane;
+  int id[ITEMS];
   const auto fetch = [&](int64_t t0) {
-    const int n = static_cast<int>(min<int64_t>(kTile, p1 - t0)), items = (n + kWg - 1) / kWg;
+    const int n = static_cast<int>(min<int64_t>(kTile, p1 - t0));
 #pragma unroll
-    for (int i = 0; i < kItems; ++i)
-      if (i < items) id[i] = ids[t0 + min(wave * 64 * items + lane + 64 * i, n - 1)];
+    for (int i = 0; i < ITEMS; ++i) id[i] = ids[t0 + min(w0 + 64 * i, n - 1)];
   };
   fetch(p0);
   __syncthreads();
@@ -148,37 +150,31 @@ __global__ __launch_bounds__(kWg) void k_dispatch_place(const int32_t* __restric
   while ((1 << bits) < E) ++bits;
   for (int64_t t0 = p0; t0 < p1; t0 += kTile) {
     const int n = static_cast<int>(min<int64_t>(kTile, p1 - t0));
-    const int items = (n + kWg - 1) / kWg;    // pairs of a lane in this tile
     for (int i = tid; i < kWaves * E; i += kWg) cnt[i] = 0;
     __syncthreads();
     int32_t* mine = cnt + wave * E;
-    const int w0 = wave * 64 * items + lane;
-    int e[kItems], rank[kItems];
+    int e[ITEMS], rank[ITEMS];
 #pragma unroll
-    for (int i = 0; i < kItems; ++i)
-      e[i] = i < items && w0 + 64 * i < n && id[i] >= 0 && id[i] < E ? id[i] : E;
+    for (int i = 0; i < ITEMS; ++i) e[i] = w0 + 64 * i < n && id[i] >= 0 && id[i] < E ? id[i] : E;
     if (t0 + kTile < p1) fetch(t0 + kTile);
 #pragma unroll
-    for (int i = 0; i < kItems; ++i) {
-      rank[i] = 0;
-      if (i < items) {
-        const bool on = e[i] < E;
-        const unsigned long long live = __ballot(on);
-        unsigned lo = static_cast<unsigned>(live), hi = static_cast<unsigned>(live >> 32);
-        for (int b = 0; b < bits; ++b) {
-          const unsigned set = -((static_cast<unsigned>(e[i]) >> b) & 1u);
-          const unsigned long long v = __ballot(set != 0);
-          lo &= ~(static_cast<unsigned>(v) ^ set);
-          hi &= ~(static_cast<unsigned>(v >> 32) ^ set);
-        }
-        const int before = __builtin_amdgcn_mbcnt_hi(hi, __builtin_amdgcn_mbcnt_lo(lo, 0));
-        rank[i] = (on ? mine[e[i]] : 0) + before;
-        // all lanes have read before the first of each expert writes; a wave's
-        // LDS accesses stay in order
-        __builtin_amdgcn_wave_barrier();
-        if (on && before == 0) mine[e[i]] = rank[i] + __popc(lo) + __popc(hi);
-        __builtin_amdgcn_wave_barrier();
+    for (int i = 0; i < ITEMS; ++i) {
+      const bool on = e[i] < E;
+      const unsigned long long live = __ballot(on);
+      unsigned lo = static_cast<unsigned>(live), hi = static_cast<unsigned>(live >> 32);
+      for (int b = 0; b < bits; ++b) {
+        const unsigned set = -((static_cast<unsigned>(e[i]) >> b) & 1u);
+        const unsigned long long v = __ballot(set != 0);
+        lo &= ~(static_cast<unsigned>(v) ^ set);
+        hi &= ~(static_cast<unsigned>(v >> 32) ^ set);
       }
+      const int before = __builtin_amdgcn_mbcnt_hi(hi, __builtin_amdgcn_mbcnt_lo(lo, 0));
+      rank[i] = (on ? mine[e[i]] : 0) + before;
+      // all lanes have read before the first of each expert writes; a wave's
+      // LDS accesses stay in order
+      __builtin_amdgcn_wave_barrier();
+      if (on && before == 0) mine[e[i]] = rank[i] + __popc(lo) + __popc(hi);
+      __builtin_amdgcn_wave_barrier();
     }
     __syncthreads();
     int run = tid < E ? seen[tid] : 0;
@@ -202,9 +198,9 @@ __global__ __launch_bounds__(kWg) void k_dispatch_place(const int32_t* __restric
       __syncthreads();
     }
 #pragma unroll
-    for (int i = 0; i < kItems; ++i) {
+    for (int i = 0; i < ITEMS; ++i) {
       const int at = w0 + 64 * i;
-      if (i < items && at < n) {
+      if (at < n) {
         const int64_t p = t0 + at;
         int place = -1;
         if (e[i] < E) {
@@ -236,31 +232,50 @@ __global__ __launch_bounds__(kWg) void k_dispatch_none(int E, int32_t* load, int
   if (threadIdx.x == 0) offsets[0] = 0;
 }
 
-// Pairs a block takes: whole waves' worth, whole tiles once it is more than one.
-int64_t chunk_of(int64_t N) {
-  const int64_t each = (N + kMaxBlocks - 1) / kMaxBlocks;
-  const int64_t unit = each <= kTile ? kWg : kTile;
-  return (each + unit - 1) / unit * unit;
+// Pairs a lane holds (1, 2, 4 or 8): the fewest that keep the blocks to
+// kMaxBlocks, or hold everything in one.
+int items_of(int64_t N) {
+  int items = 1;
+  while (items < kMaxItems && N > (int64_t)kWg * items * (N > kWg * kMaxItems ? kMaxBlocks : 1)) items *= 2;
+  return items;
 }
-int64_t blocks_of(int64_t N) { return N <= kTile ? 1 : (N + chunk_of(N) - 1) / chunk_of(N); }
+// Pairs a block takes: whole tiles.
+int64_t chunk_of(int64_t N) {
+  const int64_t tile = (int64_t)kWg * items_of(N), each = (N + kMaxBlocks - 1) / kMaxBlocks;
+  return N <= kWg * kMaxItems ? tile : (each + tile - 1) / tile * tile;
+}
+int64_t blocks_of(int64_t N) { return (N + chunk_of(N) - 1) / chunk_of(N); }
 
 }  // namespace
 
-int64_t dispatch_workspace(int64_t N, int E) { return N <= kTile ? 0 : 4 * blocks_of(N) * row_of(E); }
+int64_t dispatch_workspace(int64_t N, int E) {
+  return blocks_of(N) <= 1 ? 0 : 4 * blocks_of(N) * row_of(E);
+}
 
 hipError_t launch_dispatch(const int32_t* ids, int64_t N, int E, int64_t capacity, int32_t* load,
                            int32_t* offsets, int32_t* order, int32_t* position, void* ws,
                            hipStream_t st) {
-  const size_t lds = static_cast<size_t>(4) * kWaves * E;
   if (N == 0) {
     k_dispatch_none<<<1, kWg, 0, st>>>(E, load, offsets);
-  } else if (N <= kTile) {
-    k_dispatch_place<true><<<1, kWg, lds, st>>>(ids, N, N, E, capacity, nullptr, load, offsets, order, position);
-  } else {
-    int32_t* hist = static_cast<int32_t*>(ws);
-    const unsigned grid = static_cast<unsigned>(blocks_of(N));
-    k_dispatch_count<<<grid, kWg, 0, st>>>(ids, N, chunk_of(N), E, hist);
-    k_dispatch_place<false><<<grid, kWg, lds + kTile * 6, st>>>(ids, N, chunk_of(N), E, capacity, hist, load, offsets, order, position);
+    return hipGetLastError();
+  }
+  int32_t* hist = static_cast<int32_t*>(ws);
+  const int64_t chunk = chunk_of(N);
+  const unsigned grid = static_cast<unsigned>(blocks_of(N));
+  const auto place = [&](auto items) {
+    constexpr int I = decltype(items)::value;
+    const size_t counts = static_cast<size_t>(4) * kWaves * E;
+    if (grid == 1)
+      k_dispatch_place<true, I><<<1, kWg, counts, st>>>(ids, N, chunk, E, capacity, hist, load, offsets, order, position);
+    else
+      k_dispatch_place<false, I><<<grid, kWg, counts + kWg * I * 6, st>>>(ids, N, chunk, E, capacity, hist, load, offsets, order, position);
+  };
+  if (grid > 1) k_dispatch_count<<<grid, kWg, 0, st>>>(ids, N, chunk, E, hist);
+  switch (items_of(N)) {
+    case 1: place(std::integral_constant<int, 1>()); break;
+    case 2: place(std::integral_constant<int, 2>()); break;
+    case 4: place(std::integral_constant<int, 4>()); break;
+    default: place(std::integral_constant<int, 8>());
   }
   return hipGetLastError();
 }

@@ -22,7 +22,9 @@ constexpr int kWg = 256;
 constexpr float kNegInf = -__builtin_huge_valf();
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr int kSpan = 32;                    // experts a lane holds
-constexpr int64_t kLanesWanted = 4096 * 64;  // four waves on every SIMD
+// Four waves on every SIMD (32768 x 256 takes 17 us; with eight, in half the
+// experts a lane, 22; 65537 x 61 takes 8.3, with two 10.1, with eight 9.8).
+constexpr int64_t kLanesWanted = 4096 * 64;
 constexpr unsigned kExpTwo52 = 0x43300000u;  // high word of 2^52
 
 // ---- keys -----------------------------------------------------------------
