@@ -552,7 +552,8 @@ hipError_t launch_typed(const RouteArgs& a, hipStream_t st) {
   const int shift = lanes_shift(a.T, a.E);
   const unsigned grid = row_blocks(a.T, shift);
   const int per = a.E / a.groups, eights = per / 8, div = eights ? (65536 + eights - 1) / eights : 0;
-  const bool grouped = a.groups > 1 && a.top_groups < a.groups;
+  // (the best of the best groups of one expert are the best experts, top_groups >= top)
+  const bool grouped = per > 1 && a.top_groups < a.groups;
   by_size(a.top, [&](auto k) {
     by_size(eights_of(a.E, shift), [&](auto nb) {
       // (one code for lists of one and two; groups of any size, and long lists,

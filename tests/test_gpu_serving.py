@@ -477,6 +477,24 @@ def test_route_many_rows():
     assert bool((key[1:] > key[:-1]).all())
 
 
+@pytest.mark.parametrize("biased", [False, True])
+def test_route_groups_of_one(biased):
+    """Groups of one expert each, over enough rows that a lane holds 32 experts."""
+    import torch
+    import paper_2602_10729_amd as bo
+    _announce("route groups of one", biased)
+    T, E, top = 150_001, 64, 4
+    rng = np.random.default_rng(5)
+    few, bias, how = _route_case(rng, 300, E, "f32", biased, "sigmoid", top, E, 6, 1)
+    x = few.repeat(501, 1)[:T].contiguous()
+    b = None if bias is None else torch.from_numpy(bias).cuda()
+    r = bo.route(x, top, **{**how, "bias": b})
+    o = R.route(_np(few), top, **how)
+    want = torch.from_numpy(o["ids"]).cuda().repeat(501, 1)[:T]
+    assert torch.equal(r.ids.long(), want.long())
+    _check_route(few, bias, how, top, True, 1.0)
+
+
 # ---- dispatch ------------------------------------------------------------------
 
 @pytest.mark.parametrize("N,E", [(0, 5), (1, 1), (1, 8), (63, 3), (64, 64), (65, 7), (2048, 256),
@@ -492,6 +510,19 @@ def test_dispatch(N, E, capacity):
         ids[3], ids[5], ids[6] = E, 2 ** 31 - 1, -2 ** 31   # outside: nowhere
     d = bo.dispatch(torch.from_numpy(ids).cuda(), E, capacity=capacity)
     o = R.dispatch(ids, E, capacity)
+    for name in ("load", "offsets", "order", "position"):
+        assert np.array_equal(getattr(d, name).cpu().numpy(), o[name]), name
+
+
+def test_dispatch_most_experts_full_tiles():
+    """All experts and the largest tile, a ragged last one: the most shared memory."""
+    import torch
+    import paper_2602_10729_amd as bo
+    _announce("dispatch most experts")
+    N, E = 1_500_007, 1024
+    ids = np.random.default_rng(8).integers(-1, E + 1, N).astype(np.int32)
+    d = bo.dispatch(torch.from_numpy(ids).cuda(), E, capacity=1400)
+    o = R.dispatch(ids, E, 1400)
     for name in ("load", "offsets", "order", "position"):
         assert np.array_equal(getattr(d, name).cpu().numpy(), o[name]), name
 
