@@ -15,6 +15,14 @@
 // the threshold. A row's first chunk sets it from its lanes' maxima. What is
 // appended falls off with the place in the row, about top / chunk number a
 // chunk, so the search costs one comparison of a vector's maximum.
+//
+// What bounds it: the logits' way from memory, read once. 16897 x 128000 bf16
+// take 717 us, 6.0 TB/s (a copy of 8 GiB moves 4.7, reads and writes together).
+// A workgroup of 256 takes a row whole, four vectors of 16 bytes a lane in
+// flight. Few rows are split over workgroups by units of 8192 logits and joined
+// by a second launch: 64 x 128000 with 20 alternatives take 15 + 7 us, bound by
+// latency and barriers. One row of 32000 takes 14 us, four chunks one after the
+// other.
 #include <algorithm>
 #include <type_traits>
 
@@ -98,6 +106,17 @@ __device__ __forceinline__ int64_t xcd_order(int64_t b, int64_t each) {
   return (b % kXcds) * each + b / kXcds;
 }
 
+// Logits and gradients of more bytes than these pass the caches by (256 MB of
+// last level, and the dies' L2). A smaller gradient stays for what reads it
+// next: at 131 MB it and a product that reads it take 125 us, past the caches
+// 142, and both passes 69 against 73; at 205 MB both passes take 147 against 125,
+// at 524 MB 306 against 265 (4 of them lost again in the product).
+// The forward pass leaves its last rows for the gradient, which starts there.
+// Only where those are few does it load past the caches: both passes at 1.0 GB
+// 535 us against 544, at 2.1 GB 1086 against 1073; alone at 4.3 GB 729 against 710.
+constexpr int64_t kStreamGrad = (int64_t)160 << 20;
+constexpr int64_t kStreamForward = (int64_t)1536 << 20;
+
 struct Partial {      // of one row's share
   float M, s, w;
   int ahead;
@@ -172,7 +191,7 @@ __device__ __forceinline__ float vec_max(const Vec<TYPE>& q) {
 }
 
 // One workgroup per (row, share of the row's units).
-template <int TYPE, bool TOP>
+template <int TYPE, bool TOP, bool STREAM>
 __global__ __launch_bounds__(kWg) void k_logprobs(LogprobArgs a, int splits, int cps) {
   using El = Elem<TYPE>;
   using V = Vec<TYPE>;
@@ -199,7 +218,7 @@ __global__ __launch_bounds__(kWg) void k_logprobs(LogprobArgs a, int splits, int
       const typename El::T* xc = x + (int64_t)vb * KV;
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        q[u].load(xc + static_cast<unsigned>(min(u * kWg + tid, v1 - 1 - vb)) * KV);
+        q[u].template load<STREAM>(xc + static_cast<unsigned>(min(u * kWg + tid, v1 - 1 - vb)) * KV);
     };
     if (v0 < v1) fetch(v0);
     const int64_t tok = a.tokens ? a.tokens[row] : -1;
@@ -495,7 +514,11 @@ __global__ __launch_bounds__(kWg) void k_logprobs_join(LogprobArgs a, int splits
 //   grad_j = p_j (A + B u_j),  u_j = t - log2 s,  p_j = 2^u_j
 // streamed once, then the token's and the alternatives' terms put in place of
 // what the stream wrote there.
-template <int TYPE>
+// Bound by memory: after the forward pass over 8192 x 32000 bf16, 169 us for
+// 524 MB read and as many written, 6.2 TB/s. Rows go in the reverse of the
+// forward pass' order: what that read last is still in the last-level cache
+// (both passes 314 -> 307 us).
+template <int TYPE, bool STREAM>
 __global__ __launch_bounds__(kWg) void k_logprobs_grad(LogprobGradArgs a, int splits, int cps) {
   using El = Elem<TYPE>;
   using V = Vec<TYPE>;
@@ -505,8 +528,10 @@ __global__ __launch_bounds__(kWg) void k_logprobs_grad(LogprobGradArgs a, int sp
   const int tid = threadIdx.x;
   const int V_ = static_cast<int>(a.V), nv = V_ / KV, rest = V_ % KV;
   const float c = a.it * kLog2e;
-  const int64_t work = a.T * splits;
-  for (int64_t g = blockIdx.x; g < work; g += gridDim.x) {
+  const int64_t work = a.T * splits, each = (work + kXcds - 1) / kXcds;
+  for (int64_t b = blockIdx.x; b < each * kXcds; b += gridDim.x) {
+    const int64_t g = xcd_order(each * kXcds - 1 - b, each);
+    if (g >= work) continue;
     const int64_t row = splits == 1 ? g : g / splits;
     const int part = splits == 1 ? 0 : static_cast<int>(g - row * splits);
     const typename El::T* x = static_cast<const typename El::T*>(a.logits) + row * a.stride;
@@ -556,7 +581,7 @@ __global__ __launch_bounds__(kWg) void k_logprobs_grad(LogprobGradArgs a, int sp
     for (int vb = v0; vb < v1; vb += kWg * U) {
       V q[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) q[u].load(x + (int64_t)min(vb + u * kWg + tid, v1 - 1) * KV);
+      for (int u = 0; u < U; ++u) q[u].template load<STREAM>(x + (int64_t)min(vb + u * kWg + tid, v1 - 1) * KV);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int v = vb + u * kWg + tid;
@@ -565,7 +590,7 @@ __global__ __launch_bounds__(kWg) void k_logprobs_grad(LogprobGradArgs a, int sp
 #pragma unroll
           for (int e = 0; e < KV; ++e) r[e] = grad(q[u].get(e));
           q[u].set_all(r);
-          q[u].store(out + (int64_t)v * KV);
+          q[u].template store<STREAM>(out + (int64_t)v * KV);
         }
       }
     }
@@ -602,11 +627,28 @@ hipError_t launch(const LogprobArgs& a, hipStream_t st) {
   const Split sp = forward_split(a.T, a.V, a.top);
   const int64_t work = (a.T * sp.splits + kXcds - 1) / kXcds * kXcds;
   const dim3 grid(static_cast<unsigned>(std::min<int64_t>(work, 1 << 22)));
-  if (a.top > 0) k_logprobs<TYPE, true><<<grid, kWg, 0, st>>>(a, sp.splits, sp.cps);
-  else k_logprobs<TYPE, false><<<grid, kWg, 0, st>>>(a, sp.splits, sp.cps);
+  if (a.T * a.V * static_cast<int64_t>(type_bytes(TYPE)) > kStreamForward) {
+    if (a.top > 0) k_logprobs<TYPE, true, true><<<grid, kWg, 0, st>>>(a, sp.splits, sp.cps);
+    else k_logprobs<TYPE, false, true><<<grid, kWg, 0, st>>>(a, sp.splits, sp.cps);
+  } else {
+    if (a.top > 0) k_logprobs<TYPE, true, false><<<grid, kWg, 0, st>>>(a, sp.splits, sp.cps);
+    else k_logprobs<TYPE, false, false><<<grid, kWg, 0, st>>>(a, sp.splits, sp.cps);
+  }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || sp.splits == 1) return e;
   k_logprobs_join<TYPE><<<dim3(static_cast<unsigned>(a.T)), kWg, 0, st>>>(a, sp.splits);
+  return hipGetLastError();
+}
+
+template <int TYPE>
+hipError_t launch(const LogprobGradArgs& a, hipStream_t st) {
+  const Split sp = split_of(a.T, a.V, kMaxSplits);
+  const int64_t work = (a.T * sp.splits + kXcds - 1) / kXcds * kXcds;
+  const dim3 grid(static_cast<unsigned>(std::min<int64_t>(work, 1 << 22)));
+  if (a.T * a.V * static_cast<int64_t>(type_bytes(TYPE)) > kStreamGrad)
+    k_logprobs_grad<TYPE, true><<<grid, kWg, 0, st>>>(a, sp.splits, sp.cps);
+  else
+    k_logprobs_grad<TYPE, false><<<grid, kWg, 0, st>>>(a, sp.splits, sp.cps);
   return hipGetLastError();
 }
 
@@ -627,12 +669,9 @@ hipError_t launch_logprobs(const LogprobArgs& args, hipStream_t st) {
 }
 
 hipError_t launch_logprobs_grad(const LogprobGradArgs& a, hipStream_t st) {
-  const Split sp = split_of(a.T, a.V, kMaxSplits);
-  const dim3 grid(static_cast<unsigned>(std::min<int64_t>(a.T * sp.splits, 1 << 22)));
-  if (a.type == BO_TYPE_F32) k_logprobs_grad<BO_TYPE_F32><<<grid, kWg, 0, st>>>(a, sp.splits, sp.cps);
-  else if (a.type == BO_TYPE_BF16) k_logprobs_grad<BO_TYPE_BF16><<<grid, kWg, 0, st>>>(a, sp.splits, sp.cps);
-  else k_logprobs_grad<BO_TYPE_F16><<<grid, kWg, 0, st>>>(a, sp.splits, sp.cps);
-  return hipGetLastError();
+  if (a.type == BO_TYPE_F32) return launch<BO_TYPE_F32>(a, st);
+  if (a.type == BO_TYPE_BF16) return launch<BO_TYPE_BF16>(a, st);
+  return launch<BO_TYPE_F16>(a, st);
 }
 
 }  // namespace bo

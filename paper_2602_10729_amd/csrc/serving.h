@@ -39,9 +39,23 @@ struct Vec {
   static constexpr int kVec = 16 / sizeof(T);
   uint32_t q[4];
   // Any alignment: rows start where their stride puts them, and the memory
-  // system takes a 16-byte access at every address.
-  __device__ __forceinline__ void load(const T* p) { __builtin_memcpy(q, p, 16); }
-  __device__ __forceinline__ void store(T* p) const { __builtin_memcpy(p, q, 16); }
+  // system takes a 16-byte access at every address. STREAM: past the caches.
+  typedef uint32_t Any __attribute__((ext_vector_type(4), aligned(2)));
+  template <bool STREAM = false>
+  __device__ __forceinline__ void load(const T* p) {
+    if constexpr (STREAM) {
+      const Any v = __builtin_nontemporal_load(reinterpret_cast<const Any*>(p));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) q[i] = v[i];
+    } else {
+      __builtin_memcpy(q, p, 16);
+    }
+  }
+  template <bool STREAM = false>
+  __device__ __forceinline__ void store(T* p) const {
+    if constexpr (STREAM) __builtin_nontemporal_store(Any{q[0], q[1], q[2], q[3]}, reinterpret_cast<Any*>(p));
+    else __builtin_memcpy(p, q, 16);
+  }
   // the first n elements, the rest -inf (the first one read again)
   __device__ __forceinline__ void load_part(const T* p, int n) {
     fill_masked();

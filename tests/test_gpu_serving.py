@@ -309,6 +309,36 @@ def test_logprobs_past_32_bit_offsets():
     assert torch.equal(grad[last], alone)
 
 
+@pytest.mark.parametrize("kind,T,V,pad,shift", [("f16", 2051, 50021, 3, 1), ("bf16", 2300, 40001, 0, 5),
+                                                ("f32", 2100, 20003, 1, 3), ("f32", 4100, 100003, 2, 1)])
+def test_logprobs_past_the_caches(kind, T, V, pad, shift):
+    """Logits and gradients too large for the caches give the bits of the same
+    rows in smaller calls, whatever their stride and alignment."""
+    import torch
+    import paper_2602_10729_amd as bo
+    _announce("logprobs past the caches", kind, T, V, pad, shift)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(T)
+    buf = torch.full((T * (V + pad) + shift,), float("nan"), dtype=_dtype(kind), device="cuda")
+    x = buf[shift:].view(T, V + pad)[:, :V]
+    x.copy_(torch.randn((T, V), generator=g, device="cuda"))
+    tok = torch.randint(V, (T,), generator=g, device="cuda")
+    gl = torch.randn(T, generator=g, device="cuda")
+    # whole rows a workgroup in both (below 1024 rows they are split otherwise)
+    r = bo.token_logprobs(x, tok, top=3)
+    for a in (0, T - 1024):
+        b = slice(a, a + 1024)
+        part = bo.token_logprobs(x[b], tok[b], top=3)
+        assert all(torch.equal(u[b], v) for u, v in zip(r, part))
+    out = torch.full((T * (V + 1) + 1,), 7.0, dtype=x.dtype, device="cuda")
+    grad = bo.token_logprobs_grad(x, tok, r.stats, r.entropy, gl, gl, out=out[1:].view(T, V + 1)[:, :V])
+    assert bool((out[1:].view(T, V + 1)[:, V] == 7.0).all()) and float(out[0]) == 7.0
+    for a in range(0, T, 512):
+        b = slice(a, min(a + 512, T))
+        part = bo.token_logprobs_grad(x[b], tok[b], r.stats[b], r.entropy[b], gl[b], gl[b])
+        assert torch.equal(grad[b], part)
+
+
 # ---- routing -----------------------------------------------------------------
 
 ROUTES = [  # T, E, top, groups, top_groups, group_best
