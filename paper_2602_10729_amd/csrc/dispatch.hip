@@ -11,6 +11,9 @@
 // A tile is put in order in LDS first, so that an expert's pairs are written in
 // runs (32 of a popular tile's 8192 over 256 experts) rather than four bytes
 // here and there: 23 -> 19 us for 2.1M pairs.
+// What bounds it: a tile's chain of ballots, LDS counts and barriers, one tile a
+// compute unit: 2.1M pairs over 256 experts take 5.0 + 18.4 us (25 MB, 5.3 us at
+// a copy's rate).
 // What fits one tile takes one launch. Nothing depends on the order in which
 // atomics arrive: they only add integers.
 #include <algorithm>
