@@ -348,10 +348,12 @@ __global__ __launch_bounds__(kWg) void k_logprobs(LogprobArgs a, int splits, int
         parity ^= 1;
         if (pending + got > kCand) {
           // more than there is room for (a row that rises, or is all equal):
-          // the chunk again, 256 candidates at a time
+          // the chunk again, 256 candidates at a time (its whole vectors: what
+          // the row has past them comes on its own, and a key twice would
+          // leave a rank without one)
           kcur = merge(L, cur, kcur, pending, a.top);
           cur ^= 1;
-          const int64_t j0 = (int64_t)vb * KV, j1 = min(a.V, j0 + kWg * U * KV);
+          const int64_t j0 = (int64_t)vb * KV, j1 = min((int64_t)v1 * KV, j0 + kWg * U * KV);
           for (int64_t j = j0; j < j1; j += kWg) {
             const unsigned long long least = kcur == a.top ? L.list[cur][kcur - 1] : 0ull;
             if (j + tid < j1) {

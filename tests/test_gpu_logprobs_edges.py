@@ -1,0 +1,40 @@
+"""Log probabilities where the arithmetic and the bookkeeping of a row are at
+their edges, against the fp64 reference.
+
+Tolerances are those of the other served-output tests (see there): they follow
+from the number of roundings and hold for every value of the logits.
+"""
+import numpy as np
+import pytest
+
+from oracle import serving as R
+from test_gpu_serving import INF, _announce, _check_grad, _check_logprobs, _dtype, _logits, _np, _tokens
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("kind,V,top", [
+    ("f32", 10001, 12), ("f32", 10003, 64), ("f32", 20001, 12), ("f32", 50001, 8), ("f32", 4095, 64),
+    ("bf16", 8191, 64), ("bf16", 15001, 12), ("bf16", 32003, 20), ("bf16", 50001, 8), ("bf16", 128259, 33),
+    ("f16", 8191, 64), ("f16", 16367, 40), ("f16", 50005, 12)])
+def test_alternatives_of_a_full_last_chunk(kind, V, top):
+    """More candidates in a row's last chunk than there is room for, with logits
+    behind its whole vectors: every alternative once."""
+    import torch
+    import paper_2602_10729_amd as bo
+    _announce("alternatives of a full last chunk", kind, V, top)
+    rng = np.random.default_rng(V)
+    T = 24
+    x = _logits(rng, T, V, kind)
+    x[0] = torch.linspace(-4, 4, V, device="cuda")         # rising: the last chunk holds the best
+    x[1] = x[0].flip(0)
+    x[2, : V - 900] = -INF                                 # live at the end only
+    x[3, : V - 900] = -INF
+    x[3, V - 1] = 30.0                                     # the very last is the likeliest
+    x[4, : V - 900] = -20.0
+    x[5] = 0.25                                            # all equal
+    x[6, : V - 5] = -INF
+    x[7, -9:] += 50.0
+    tok = rng.integers(0, V, T)
+    r = bo.token_logprobs(x, _tokens(tok), top=top)
+    _check_logprobs(r, x, tok, top, 1.0)
