@@ -226,7 +226,9 @@ __global__ __launch_bounds__(kWg) void k_logprobs(LogprobArgs a, int splits, int
     const float xt = has ? El::load(x[tok]) : 0.0f;
     // what a logit must exceed to stand before the token: behind it and ahead
     const float gt = has ? xt : __builtin_huge_valf(), ge = has ? below(xt) : gt;
-    const int tv = has ? static_cast<int>(tok) / KV : -1;  // the token's vector
+    // the token's vector (nv past the whole ones: then every vector is ahead of it,
+    // and the logits before it in the rest are counted there)
+    const int tv = has ? static_cast<int>(tok) / KV : -1;
 
     // the lane's reference: itself, as it is subtracted (0 for none), scaled, and
     // what a logit must exceed to move it
@@ -307,7 +309,7 @@ __global__ __launch_bounds__(kWg) void k_logprobs(LogprobArgs a, int splits, int
           }
           if (!FIRST) continue;
           m = max2(m, vm);
-          if (v == tv) {                                   // one lane of one chunk
+          if (v == tv && v < v1) {                         // one lane of one chunk
             for (int64_t j = (int64_t)v * KV; j < tok; ++j) ahead_lane += El::load(x[j]) == xt;
           }
           if (TOP && __any(!(vm <= th))) {

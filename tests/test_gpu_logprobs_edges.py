@@ -38,3 +38,22 @@ def test_alternatives_of_a_full_last_chunk(kind, V, top):
     tok = rng.integers(0, V, T)
     r = bo.token_logprobs(x, _tokens(tok), top=top)
     _check_logprobs(r, x, tok, top, 1.0)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("base", [0, 512, 1000, 8192, 40960])
+def test_rank_of_tied_tokens_past_the_vectors(kind, base):
+    """Equal logits before a token count once each, wherever in the row it stands:
+    every length of what is left past the whole vectors, every place in it."""
+    import torch
+    import paper_2602_10729_amd as bo
+    _announce("rank of tied tokens", kind, base)
+    rng = np.random.default_rng(base)
+    for rest in range(1, 9):
+        V = base + rest
+        T = 2 * min(V, 12)
+        x = torch.full((T, V), 0.5, device="cuda").to(_dtype(kind))
+        x[T // 2:] = torch.from_numpy(rng.integers(0, 3, (T - T // 2, V)).astype(np.float32)).cuda().to(x.dtype)
+        tok = V - 1 - np.arange(T) % (T // 2)
+        r = bo.token_logprobs(x, _tokens(tok))
+        _check_logprobs(r, x, tok, 0, 1.0)
