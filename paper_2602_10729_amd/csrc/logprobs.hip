@@ -181,13 +181,25 @@ __device__ int merge(TopLds& L, int cur, int kcur, int n, int k) {
   return all < k ? all : k;
 }
 
+// A vector's largest logit, NaN where it holds one: a maximum that drops NaN
+// turns a signalling one into a quiet one first, and what it was compared with
+// is dropped with it by the next.
 template <int TYPE>
 __device__ __forceinline__ float vec_max(const Vec<TYPE>& q) {
-  if constexpr (Vec<TYPE>::kVec == 8)
-    return max2(max3(q.get(0), q.get(1), q.get(2)),
-                max3(q.get(3), q.get(4), max3(q.get(5), q.get(6), q.get(7))));
-  else
-    return max2(max3(q.get(0), q.get(1), q.get(2)), q.get(3));
+  if constexpr (Vec<TYPE>::kVec == 8) {
+    const float low = max3_nan(q.get(0), q.get(1), q.get(2));
+    return max3_nan(low, max3_nan(q.get(3), q.get(4), q.get(5)), max3_nan(q.get(6), q.get(7), low));
+  } else {
+    return max3_nan(max3_nan(q.get(0), q.get(1), q.get(2)), q.get(3), q.get(3));
+  }
+}
+// The largest of a vector that holds NaN (-inf when it holds nothing else).
+template <int TYPE>
+__device__ __forceinline__ float vec_max_beside_nan(const Vec<TYPE>& q) {
+  float m = kNegInf;
+#pragma unroll
+  for (int e = 0; e < Vec<TYPE>::kVec; ++e) m = q.get(e) > m ? q.get(e) : m;
+  return m;
 }
 
 // One workgroup per (row, share of the row's units).
@@ -286,10 +298,13 @@ __global__ __launch_bounds__(kWg) void k_logprobs(LogprobArgs a, int splits, int
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           if (vb + u * kWg + wave * 64 >= v1) break;
-          const float vm = vec_max<TYPE>(q[u]);
-          if (vm > lim) {
-            move_to(vm, ref, c, s, w);
-            set_ref(vm);
+          float vm = vec_max<TYPE>(q[u]);
+          if (!(vm <= lim)) {
+            if (vm != vm) vm = vec_max_beside_nan<TYPE>(q[u]);
+            if (vm > lim) {
+              move_to(vm, ref, c, s, w);
+              set_ref(vm);
+            }
           }
           const int v = vb + u * kWg + tid;
           const float thr = v < tv ? ge : gt;
@@ -393,7 +408,7 @@ __global__ __launch_bounds__(kWg) void k_logprobs(LogprobArgs a, int splits, int
         move_to(lr, ref, c, s, w);
         set_ref(lr);
       }
-      m = max2(m, lr);
+      m = lr > m ? lr : m;
       const float t = fmaf(lr - rz, c, fabsf(rz) < kFar ? fmaf(rz, c, -R) : 0.0f);
       const float ex = __builtin_amdgcn_exp2f(t);
       s += ex;

@@ -161,12 +161,13 @@ __device__ __forceinline__ int key_index(unsigned long long k) {
   return static_cast<int>(0xFFFFFFFFu - static_cast<unsigned>(k));
 }
 
-// max of three; NaN operands are dropped (a signalling one may come through)
-__device__ __forceinline__ float max3(float a, float b, float c) {
+// max of three, NaN if one of them is
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
   float d;
-  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
+  asm("v_maximum3_f32 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
   return d;
 }
+// max of two; a quiet NaN operand is dropped (a signalling one comes through quiet)
 __device__ __forceinline__ float max2(float a, float b) {
   float d;
   asm("v_max_f32 %0, %1, %2" : "=v"(d) : "v"(a), "v"(b));

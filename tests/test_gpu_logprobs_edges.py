@@ -57,3 +57,37 @@ def test_rank_of_tied_tokens_past_the_vectors(kind, base):
         tok = V - 1 - np.arange(T) % (T // 2)
         r = bo.token_logprobs(x, _tokens(tok))
         _check_logprobs(r, x, tok, 0, 1.0)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("V", [700, 9000, 50003])
+def test_rank_beside_signalling_nans(kind, V):
+    """A logit above the token's counts, also where a NaN of any kind stands
+    beside it and nothing else in reach is above the token."""
+    import torch
+    import paper_2602_10729_amd as bo
+    _announce("rank beside NaN", kind, V)
+    rng = np.random.default_rng(31)
+    word, bits = {"f32": (torch.int32, [0x7F800001, 0x7FC00000, -0x7FFFFF, -1]),
+                  "bf16": (torch.int16, [0x7F81, 0x7FC0, -0x7F, -1]),
+                  "f16": (torch.int16, [0x7C01, 0x7E00, -0x3FF, -1])}[kind]
+    T = 32
+    x = _logits(rng, T, V, kind)
+    tok = rng.integers(0, V, T)
+    for t in range(T):
+        at = 16 * int(rng.integers(0, (V - 16) // 16)) + t % 8      # a vector's every place
+        x[t, tok[t]] = 20.0
+        nan = 16 * (at // 16) + (t // 4) % 8
+        if tok[t] // 16 == at // 16:
+            tok[t] = (tok[t] + 32) % (V - 16)
+            x[t, tok[t]] = 20.0
+        x[t, at] = 30.0
+        if nan == at:
+            nan = at ^ 1
+        x[t].view(word)[nan] = bits[t % 4]
+    o = R.token_logprobs(_np(x), tok, 2)
+    for top in (0, 2):
+        r = bo.token_logprobs(x, _tokens(tok), top=top)
+        assert np.array_equal(r.rank.cpu().numpy(), o["rank"])
+        assert bool(r.logprob.isnan().all()) and np.array_equal(_np(r.stats[:, 0]), o["stats"][:, 0])
+    assert np.array_equal(r.top_ids.cpu().numpy(), o["top_ids"])
