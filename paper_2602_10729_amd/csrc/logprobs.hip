@@ -7,8 +7,11 @@
 // joined by moving their sums to the row's maximum M:
 //   s' = s 2^d,  w' = (w + d s) 2^d,  d = R - R_M;
 // what R_M lost in rounding, c M - R_M, goes back into the logarithm of the
-// sum. A masked logit makes t 2^t NaN: a chunk that ends with w not finite is
-// summed again with t bounded from below, and the wave stays on that path.
+// sum. A masked logit makes t 2^t NaN, and so does a reference so far from 0
+// (|c r| >= 2^24) that R says nothing about the last bits of an exponent: a chunk
+// that ends with w not finite is summed again with t = c (l - r) + (c r - R), the
+// second term 0 for a far reference, t bounded from below in the product; the
+// wave stays on that path.
 // The largest logits are collected on the way: a workgroup knows a threshold
 // that at least `top` logits of the row reach, appends what lies above it to a
 // list in LDS, and now and then keeps the list's `top` best, whose last raises
@@ -77,21 +80,34 @@ __device__ __forceinline__ float wave_sum(float v) {
   return wave_reduce(v, 0.0f, [](float p, float q) { return p + q; });
 }
 
-// References this large (the type's lowest value) leave fp32 when scaled.
-constexpr float kFar = 1e37f;
-// (Rounded by itself: contracted into what uses it, the lanes' references would
-// no longer be the ones that their sums are relative to.)
+// A scaled reference, NaN from 2^24 on: there its rounding is more than a unit of
+// an exponent (a mask of -1e10 would be off by 2^100), so a lane with such a
+// reference has to take differences first, t = c (l - r); the NaN in its sums
+// tells the wave. (Rounded by itself: contracted into what uses it, the lanes'
+// references would no longer be the ones that their sums are relative to.)
+constexpr float kNear = 16777216.0f;
 __device__ __forceinline__ float scaled_ref(float r, float c) {
 #pragma clang fp contract(off)
-  return fabsf(r) < kFar ? r * c : 0.0f;
+  const float R = r * c;
+  return fabsf(R) < kNear ? R : __builtin_nanf("");
+}
+// What R = scaled_ref(r, c) lost in rounding: sums are relative to c r - lost.
+__device__ __forceinline__ float lost_of(float r, float c, float R) {
+  return R == R ? fmaf(r, c, -R) : 0.0f;
+}
+// c (a - b), of halves: a - b may leave fp32 where c (a - b) does not.
+__device__ __forceinline__ float scaled_diff(float a, float b, float c) {
+  return fmaf(a, 0.5f, -0.5f * b) * (2.0f * c);
 }
 // (s, w) relative to r, moved to M >= r: a lane without a finite logit has
 // r = -inf and s = 0 (or NaN, which stays).
 __device__ __forceinline__ void move_to(float M, float r, float c, float& s, float& w) {
 #pragma clang fp contract(off)
   if (r == kNegInf) return;
-  float d = scaled_ref(r, c) - scaled_ref(M, c);
-  if (!(fabsf(r) < kFar && fabsf(M) < kFar)) d = fmaxf((r - M) * c, kLow);
+  const float Rr = scaled_ref(r, c), RM = scaled_ref(M, c);
+  float d = Rr - RM;
+  // (bounded, so that s d stays finite where it is multiplied by 0)
+  if (d != d) d = fmaxf(scaled_diff(r, M, c) + (lost_of(M, c, RM) - lost_of(r, c, Rr)), -1e4f);
   const float f = __builtin_amdgcn_exp2f(d);
   w = (w + s * d) * f;
   s *= f;
@@ -127,13 +143,13 @@ __device__ __forceinline__ float finish(const LogprobArgs& a, int64_t row, const
                                         int64_t tok, float xt) {
   const bool has = tok >= 0 && tok < a.V;
   const float c = a.c;
-  const float lost = fabsf(p.M) < kFar ? fmaf(p.M, c, -scaled_ref(p.M, c)) : 0.0f;
+  const float lost = lost_of(p.M, c, scaled_ref(p.M, c));
   const float ls0 = logf(p.s), ls = ls0 - lost * kLn2;
   a.stats[2 * row] = p.M;
   a.stats[2 * row + 1] = ls;
   a.entropy[row] = p.M == kNegInf && p.s == 0.0f ? 0.0f : ls0 - p.w / p.s * kLn2;
   float lp = 0.0f;
-  if (has) lp = xt == kNegInf && p.s == p.s ? kNegInf : (xt - p.M) * a.it - ls;
+  if (has) lp = xt == kNegInf && p.s == p.s ? kNegInf : scaled_diff(xt, p.M, a.it) - ls;
   if (tok >= a.V) lp = __builtin_nanf("");
   a.logprob[row] = lp;
   a.rank[row] = has && xt > kNegInf ? p.ahead + 1 : 0;
@@ -142,7 +158,7 @@ __device__ __forceinline__ float finish(const LogprobArgs& a, int64_t row, const
 __device__ __forceinline__ void finish_top(const LogprobArgs& a, int64_t row, int i,
                                            unsigned long long key, float M, float ls) {
   a.top_ids[row * a.top + i] = key ? key_index(key) : -1;
-  a.top_logprobs[row * a.top + i] = key ? (key_value(key) - M) * a.it - ls : kNegInf;
+  a.top_logprobs[row * a.top + i] = key ? scaled_diff(key_value(key), M, a.it) - ls : kNegInf;
 }
 
 struct alignas(16) TopLds {
@@ -242,8 +258,8 @@ __global__ __launch_bounds__(kWg) void k_logprobs(LogprobArgs a, int splits, int
     // and the logits before it in the rest are counted there)
     const int tv = has ? static_cast<int>(tok) / KV : -1;
 
-    // the lane's reference: itself, as it is subtracted (0 for none), scaled, and
-    // what a logit must exceed to move it
+    // the lane's reference: itself, as it is subtracted (0 for none), scaled (NaN
+    // when it is far from 0), and what a logit must exceed to move it
     float m = kNegInf, ref = kNegInf, rz = 0.0f, R = 0.0f, lim = kNegInf, s = 0.0f, w = 0.0f;
     const auto set_ref = [&](float r) {
       ref = rz = r;
@@ -251,7 +267,7 @@ __global__ __launch_bounds__(kWg) void k_logprobs(LogprobArgs a, int splits, int
       lim = r + slack;
     };
     int ahead = 0, ahead_lane = 0;
-    bool bounded = false;                      // the row has met a masked logit (per wave)
+    bool bounded = false;                      // the row has met a masked or far logit (per wave)
     float th = kNegInf;
     int cur = 0, kcur = 0, pending = 0, parity = 0;
     int seen[2] = {0, 0};
@@ -308,7 +324,7 @@ __global__ __launch_bounds__(kWg) void k_logprobs(LogprobArgs a, int splits, int
           }
           const int v = vb + u * kWg + tid;
           const float thr = v < tv ? ge : gt;
-          const float off = BOUNDED && fabsf(rz) < kFar ? fmaf(rz, c, -R) : 0.0f;
+          const float off = BOUNDED ? lost_of(rz, c, R) : 0.0f, half = -0.5f * rz;
           // (a token among its row's likeliest: few vectors hold what precedes it)
           if (FIRST && __any(vm > thr)) {
 #pragma unroll
@@ -317,7 +333,7 @@ __global__ __launch_bounds__(kWg) void k_logprobs(LogprobArgs a, int splits, int
 #pragma unroll
           for (int e = 0; e < KV; ++e) {
             const float l = q[u].get(e);
-            const float t = BOUNDED ? fmaf(l - rz, c, off) : fmaf(l, c, -R);
+            const float t = BOUNDED ? fmaf(fmaf(l, 0.5f, half), 2.0f * c, off) : fmaf(l, c, -R);
             const float ex = __builtin_amdgcn_exp2f(t);
             s += ex;
             w = fmaf(ex, BOUNDED ? max2(t, kLow) : t, w);
@@ -409,7 +425,7 @@ __global__ __launch_bounds__(kWg) void k_logprobs(LogprobArgs a, int splits, int
         set_ref(lr);
       }
       m = lr > m ? lr : m;
-      const float t = fmaf(lr - rz, c, fabsf(rz) < kFar ? fmaf(rz, c, -R) : 0.0f);
+      const float t = scaled_diff(lr, rz, c) + lost_of(rz, c, R);
       const float ex = __builtin_amdgcn_exp2f(t);
       s += ex;
       w = fmaf(ex, max2(t, kLow), w);
@@ -558,7 +574,7 @@ __global__ __launch_bounds__(kWg) void k_logprobs_grad(LogprobGradArgs a, int sp
     const int v0 = min(nv, part * cps * (kUnit / KV)), v1 = min(nv, v0 + cps * (kUnit / KV));
     const float m0 = a.stats[2 * row], ls0 = a.stats[2 * row + 1];
     const bool empty = m0 == kNegInf && ls0 == kNegInf;
-    const float m = empty ? 0.0f : m0, ls2 = empty ? 0.0f : ls0 * kLog2e;
+    const float half = empty ? 0.0f : -0.5f * m0, ls2 = empty ? 0.0f : ls0 * kLog2e;
     const int64_t tok = a.tokens ? a.tokens[row] : -1;
     const bool has = tok >= 0 && tok < a.V;
     const float gl = has && a.g_logprob ? a.g_logprob[row] : 0.0f;
@@ -594,7 +610,7 @@ __global__ __launch_bounds__(kWg) void k_logprobs_grad(LogprobGradArgs a, int sp
     if (tok >= a.V) A = __builtin_nanf("");
     if (empty) A = B = 0.0f;
     const auto grad = [&](float l) {
-      const float u = fmaf(l - m, c, -ls2);
+      const float u = fmaf(fmaf(l, 0.5f, half), 2.0f * c, -ls2);   // c (l - m) - log2 s
       return __builtin_amdgcn_exp2f(u) * fmaf(B, max2(u, kLow), A);
     };
     for (int vb = v0; vb < v1; vb += kWg * U) {

@@ -91,3 +91,80 @@ def test_rank_beside_signalling_nans(kind, V):
         assert np.array_equal(r.rank.cpu().numpy(), o["rank"])
         assert bool(r.logprob.isnan().all()) and np.array_equal(_np(r.stats[:, 0]), o["stats"][:, 0])
     assert np.array_equal(r.top_ids.cpu().numpy(), o["top_ids"])
+
+
+# 131077 = 16 * 8192 + 5: a row's last share is what is left past the vectors
+@pytest.mark.parametrize("V", [40, 3001, 50003, 131077])
+@pytest.mark.parametrize("kind,mask", [("f32", -1e10), ("f32", -1e20), ("f32", -1e30), ("f32", -1e35), ("f32", "lowest"),
+                                       ("bf16", -1e10), ("bf16", -1e20), ("bf16", -1e30), ("bf16", "lowest"),
+                                       ("f16", -6e4), ("f16", "lowest")])
+def test_logprobs_finite_masks(V, kind, mask):
+    """Masks that are large finite values: in part of a row, in whole shares of
+    it, in all of it, beside -inf, and as the given token."""
+    import torch
+    import paper_2602_10729_amd as bo
+    _announce("logprobs finite masks", V, kind, mask)
+    rng = np.random.default_rng(V)
+    T, top = 9, 12
+    x = _logits(rng, T, V, kind)
+    value = torch.finfo(x.dtype).min if mask == "lowest" else mask
+    cut = torch.from_numpy(rng.random(V) < 0.9).cuda()
+    x[0, cut] = value
+    x[1] = value                                   # uniform over the mask
+    x[2] = value
+    x[2, V - 1] = 1.5                              # one live, at the end
+    x[3, : V // 2] = value
+    x[4, 5:] = value
+    x[5, cut] = value
+    x[5, ::3] = -INF
+    x[6] = x[6] * (-value / 16)                     # as far apart as the mask is far
+    x[7, V // 2] = -value                          # one above all others
+    x[8] = -INF
+    x[8, ::2] = value
+    tok = rng.integers(0, V, T)
+    tok[0], tok[2], tok[3], tok[7] = int(cut.nonzero()[0]), V - 1, 0, V // 2
+    for it in (0.5, 2 / 3, 1.0, 2.0):
+        r = bo.token_logprobs(x, _tokens(tok), top=top, inv_temperature=it)
+        _check_logprobs(r, x, tok, top, it)
+        _check_grad(x, tok, r, rng, it, top, kind)
+
+
+@pytest.mark.parametrize("V", [3001, 50003])
+def test_logprobs_offsets_of_every_size(V):
+    """Rows that lie around every power of four from 1 to 2^62, and around the
+    place where a scaled logit stops being exact to a unit (2^24)."""
+    import torch
+    import paper_2602_10729_amd as bo
+    _announce("logprobs offsets of every size", V)
+    rng = np.random.default_rng(V + 1)
+    centres = [s * 4.0 ** k for k in range(32) for s in (1, -1)] + [s * 11629080.0 for s in (1, -1)]
+    x = _logits(rng, len(centres), V, "f32", spread=3.0)
+    x += torch.tensor(centres, dtype=torch.float32, device="cuda")[:, None]
+    tok = rng.integers(0, V, len(centres))
+    for it in (1.0, 1 / 0.7):
+        r = bo.token_logprobs(x, _tokens(tok), top=3, inv_temperature=it)
+        _check_logprobs(r, x, tok, 3, it)
+        _check_grad(x, tok, r, rng, it, 3, "f32")
+
+
+@pytest.mark.parametrize("V", [700, 40003])
+@pytest.mark.parametrize("kind,it", [("f32", 1e9), ("f32", 1e30), ("bf16", 1e9), ("bf16", 1e30), ("f16", 1e4),
+                                     ("f32", 1e-20), ("f32", 1e-38), ("f32", 1e-40), ("bf16", 1e-38)])
+def test_logprobs_extreme_temperatures(V, kind, it):
+    import torch
+    import paper_2602_10729_amd as bo
+    _announce("logprobs extreme temperatures", V, kind, it)
+    rng = np.random.default_rng(V + 2)
+    x = _logits(rng, 6, V, kind)
+    low = torch.finfo(x.dtype).min
+    x[1, ::2] = low
+    x[2, ::2] = low
+    x[2, 1::4] = -low                              # apart by more than the type's largest value
+    x[3, : V // 2] = -INF
+    x[4] = low
+    x[5] = -INF
+    tok = rng.integers(0, V, 6)
+    r = bo.token_logprobs(x, _tokens(tok), top=5, inv_temperature=it)
+    _check_logprobs(r, x, tok, 5, it)
+    if it < 1e29:                                  # (beyond, terms of a gradient leave fp32)
+        _check_grad(x, tok, r, rng, it, 5, kind, use=(True, it < 1, True))
