@@ -609,9 +609,12 @@ __global__ __launch_bounds__(kWg) void k_logprobs_grad(LogprobGradArgs a, int sp
     float A = a.it * (-total - gh * a.entropy[row]), B = -a.it * gh * kLn2;
     if (tok >= a.V) A = __builtin_nanf("");
     if (empty) A = B = 0.0f;
+    // where p is 0: no product with what may be infinite, NaN only as A's
+    const float none = A != A ? A : 0.0f;
     const auto grad = [&](float l) {
       const float u = fmaf(fmaf(l, 0.5f, half), 2.0f * c, -ls2);   // c (l - m) - log2 s
-      return __builtin_amdgcn_exp2f(u) * fmaf(B, max2(u, kLow), A);
+      const float p = __builtin_amdgcn_exp2f(u);
+      return p == 0.0f ? none : p * fmaf(B, u, A);
     };
     for (int vb = v0; vb < v1; vb += kWg * U) {
       V q[U];

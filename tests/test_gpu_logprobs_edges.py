@@ -168,3 +168,35 @@ def test_logprobs_extreme_temperatures(V, kind, it):
     _check_logprobs(r, x, tok, 5, it)
     if it < 1e29:                                  # (beyond, terms of a gradient leave fp32)
         _check_grad(x, tok, r, rng, it, 5, kind, use=(True, it < 1, True))
+
+
+@pytest.mark.parametrize("kind,it,size", [("f32", 1.0, 1e9), ("f32", 1e9, 1.0), ("f32", 1e30, 1.0), ("f32", 1e30, 1e6),
+                                          ("bf16", 1.0, 1e9), ("bf16", 1e9, 1.0), ("f32", 1.0, 3e38)])
+def test_gradient_of_impossible_tokens_is_zero(kind, it, size):
+    """Masked logits, and those whose probability is 0 in fp32, have gradient 0
+    however large the incoming gradients are; NaN still reaches the whole row."""
+    import torch
+    import paper_2602_10729_amd as bo
+    _announce("gradient of impossible tokens", kind, it, size)
+    rng = np.random.default_rng(4)
+    T, V = 4, 9003
+    x = _logits(rng, T, V, kind)
+    x[1, ::2] = -INF
+    x[2, ::2] = -1e30
+    x[3, 1:] = -1e4
+    x[3, 0] = 0.0
+    tok = np.array([7, 1, 3, 0])
+    r = bo.token_logprobs(x, _tokens(tok), inv_temperature=it)
+    sized = torch.full((T,), size, device="cuda")
+    l = _np(x)
+    off = torch.from_numpy((l - l.max(1, keepdims=True)) * float(np.float32(it)) < -200.0).cuda()
+    off[torch.arange(T), _tokens(tok)] = False     # (a token has its own term)
+    for gl, gh in ((None, sized), (sized, None), (sized, sized), (sized, -sized)):
+        g = bo.token_logprobs_grad(x, _tokens(tok), r.stats, r.entropy, gl, gh, inv_temperature=it)
+        assert bool((g[off] == 0).all())
+    nan = torch.full((T,), float("nan"), device="cuda")
+    for gl, gh in ((nan, None), (None, nan)):
+        g = bo.token_logprobs_grad(x, _tokens(tok), r.stats, r.entropy, gl, gh, inv_temperature=it)
+        assert bool(g.isnan().all())
+    past = bo.token_logprobs_grad(x, _tokens([V, V, V, V]), r.stats, r.entropy, sized, inv_temperature=it)
+    assert bool(past.isnan().all())
