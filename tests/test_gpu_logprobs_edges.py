@@ -200,3 +200,42 @@ def test_gradient_of_impossible_tokens_is_zero(kind, it, size):
         assert bool(g.isnan().all())
     past = bo.token_logprobs_grad(x, _tokens([V, V, V, V]), r.stats, r.entropy, sized, inv_temperature=it)
     assert bool(past.isnan().all())
+
+
+@pytest.mark.parametrize("V,top", [(40001, 12), (81923, 64), (131077, 5), (131077, 64)])
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+def test_logprobs_joined_shares(V, top, kind):
+    """Rows shared out over workgroups: shares with no live logit, with NaN or an
+    infinity, with the only live ones, and a last one that holds only what is
+    left past the vectors."""
+    import torch
+    import paper_2602_10729_amd as bo
+    _announce("logprobs joined shares", V, top, kind)
+    rng = np.random.default_rng(V + top)
+    T, S = 16, 8192
+    x = _logits(rng, T, V, kind)
+    low = torch.finfo(x.dtype).min
+    tok = rng.integers(0, V, T)
+    x[0] = -INF                                    # nothing left
+    x[1, :S] = -INF                                # a share masked
+    x[2, S:] = -INF                                # all but a share
+    x[3] = -INF
+    x[3, V - 1] = -7.0                             # one left, at the very end
+    x[4] = -INF
+    x[4, S - 1] = 3.0                              # one left, at a share's end
+    x[5] = low
+    x[6, : 2 * S] = low
+    x[7, S + 5] = float("nan")
+    x[8, 2 * S + 9] = INF
+    x[9] = 0.5
+    x[10] = torch.linspace(-8, 8, V, device="cuda")        # each share above the one before
+    x[11] = x[10].flip(0)
+    x[12, : V - 3] = -INF                          # fewer than top
+    x[13, S: 3 * S] = low
+    x[13, 3 * S:] = -INF
+    x[14, V - 2] = 50.0
+    tok[2], tok[3], tok[4], tok[12], tok[14], tok[15] = S - 1, V - 1, S - 1, V - 2, V - 2, -1
+    for it in (1.0, 0.5):
+        r = bo.token_logprobs(x, _tokens(tok), top=top, inv_temperature=it)
+        _check_logprobs(r, x, tok, top, it)
+        _check_grad(x, tok, r, rng, it, top, kind)
