@@ -549,6 +549,9 @@ bo_status bo_measure_peak(int32_t what, int64_t iters, double* rate, void* strea
  * Sums are held in fp32, partial sums per lane; the order of summation is
  * fixed, so a call repeats bit for bit.
  *
+ * Finite logits of every size are taken at their value, also the large negative
+ * ones that stand for masks. Probabilities below fp32's normal range (2^-126) are
+ * 0, and so is their part of a gradient.
  * A logit of -inf is masked: probability 0, no rank, never an alternative.
  * Alternatives that a row lacks are index -1, log probability -inf. A row
  * with every logit masked gives logprob -inf, rank 0, entropy 0, stats
@@ -570,8 +573,8 @@ bo_status bo_measure_peak(int32_t what, int64_t iters, double* rate, void* strea
  *          bo_token_logprobs_workspace(T, V, top) bytes (NULL when that is 0);
  *          overwritten; calls that may overlap need one each
  * T >= 0 (0 is a no-op), 1 <= V < 2^31.
- * Asynchronous. Errors: INVALID_ARGUMENT, CAPACITY (top, V, T * splits past
- * the grid), DEVICE.
+ * Asynchronous. Errors: INVALID_ARGUMENT, CAPACITY (top, V or T beyond its
+ * limit, or an extent past 2^63 bytes), DEVICE.
  */
 int64_t bo_token_logprobs_workspace(int64_t T, int64_t V, int32_t top);
 bo_status bo_token_logprobs(const void* logits, int32_t type, int64_t T, int64_t V,

@@ -439,6 +439,9 @@ def draw_fronts3_test(F, ref, lower=None, stream=None):
 
 
 # ---- served outputs: log probabilities, routing, dispatch ----------------------
+#
+# None of these calls takes part in torch's autograd: what they return requires no
+# gradient, whatever their inputs do. Gradients come from the _grad calls.
 
 class TokenLogprobs(NamedTuple):
     """What token_logprobs returns, row by row: fp32 ``logprob``, ``entropy``
@@ -535,7 +538,8 @@ def _workspace(t, stream, nbytes):
 def token_logprobs(logits, tokens=None, top=0, inv_temperature=1.0, out=None, stream=None):
     """bo_token_logprobs: logits [T, V] (fp32, bf16 or fp16 GPU tensor, rows
     any distance apart), tokens int64 [T] (negative: none) or None. Returns a
-    TokenLogprobs; ``out`` takes one of the same shapes to write into."""
+    TokenLogprobs; ``out`` takes one of the same shapes to write into. Outside
+    autograd: the logits' gradient is token_logprobs_grad's."""
     lp, kind, T, V, stride = _rows(logits, "logits")
     top = int(top)
     if top < 0:
@@ -603,7 +607,8 @@ def route(logits, top, bias=None, score="softmax", groups=1, top_groups=1, group
     enters the choice only (-inf withdraws an expert); with groups the choice
     is limited to the ``top_groups`` best groups, by the sum of their
     ``group_best`` largest values. Returns a Routing; ``out`` takes one of the
-    same shapes to write into."""
+    same shapes to write into. Outside autograd: the logits' gradient is
+    route_grad's."""
     lp, kind, T, E, stride = _rows(logits, "logits")
     top = int(top)
     if top < 1:

@@ -20,10 +20,10 @@
 // chunk, so the search costs one comparison of a vector's maximum.
 //
 // What bounds it: the logits' way from memory, read once. 16897 x 128000 bf16
-// take 717 us, 6.0 TB/s (a copy of 8 GiB moves 4.7, reads and writes together).
+// take 729 us, 5.9 TB/s (a copy of 4 GiB moves 4.7, reads and writes together).
 // A workgroup of 256 takes a row whole, four vectors of 16 bytes a lane in
 // flight. Few rows are split over workgroups by units of 8192 logits and joined
-// by a second launch: 64 x 128000 with 20 alternatives take 15 + 7 us, bound by
+// by a second launch: 64 x 128000 with 20 alternatives take 16 + 7 us, bound by
 // latency and barriers. One row of 32000 takes 14 us, four chunks one after the
 // other.
 #include <algorithm>
@@ -124,12 +124,12 @@ __device__ __forceinline__ int64_t xcd_order(int64_t b, int64_t each) {
 
 // Logits and gradients of more bytes than these pass the caches by (256 MB of
 // last level, and the dies' L2). A smaller gradient stays for what reads it
-// next: at 131 MB it and a product that reads it take 125 us, past the caches
-// 142, and both passes 69 against 73; at 205 MB both passes take 147 against 125,
-// at 524 MB 306 against 265 (4 of them lost again in the product).
+// next: at 131 MB it and a product that reads it take 128 us, past the caches
+// 144, and both passes 71 against 74; at 205 MB both passes take 147 against 125,
+// at 524 MB 307 against 267 (4 of them lost again in the product).
 // The forward pass leaves its last rows for the gradient, which starts there.
 // Only where those are few does it load past the caches: both passes at 1.0 GB
-// 535 us against 544, at 2.1 GB 1086 against 1073; alone at 4.3 GB 729 against 710.
+// 544 us against 557, at 2.1 GB 1087 against 1081; alone at 4.3 GB 747 against 729.
 constexpr int64_t kStreamGrad = (int64_t)160 << 20;
 constexpr int64_t kStreamForward = (int64_t)1536 << 20;
 
@@ -549,8 +549,8 @@ __global__ __launch_bounds__(kWg) void k_logprobs_join(LogprobArgs a, int splits
 //   grad_j = p_j (A + B u_j),  u_j = t - log2 s,  p_j = 2^u_j
 // streamed once, then the token's and the alternatives' terms put in place of
 // what the stream wrote there.
-// Bound by memory: after the forward pass over 8192 x 32000 bf16, 169 us for
-// 524 MB read and as many written, 6.2 TB/s. Rows go in the reverse of the
+// Bound by memory: after the forward pass over 8192 x 32000 bf16, 167 us for
+// 524 MB read and as many written, 6.3 TB/s. Rows go in the reverse of the
 // forward pass' order: what that read last is still in the last-level cache
 // (both passes 314 -> 307 us).
 template <int TYPE, bool STREAM>
