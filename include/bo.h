@@ -29,6 +29,10 @@
  *               answers, the router's choices and their grouping by model
  *               ("Threshold router", load fractions and load distribution),
  *               with the gradients that train the model and the router.
+ *   bo_linear_logprobs, bo_expert_gather / bo_expert_combine, bo_embed — the
+ *               served model's own ends and expert layers: log probabilities
+ *               straight from hidden rows, tokens to their experts' rows and
+ *               back, rows of an embedding table; all with their gradients.
  *
  * Conventions shared by every entry point:
  *   - All floating-point arrays are fp32, row-major, contiguous, unless an
@@ -514,7 +518,8 @@ bo_status bo_profile_read(double* posterior_ms, double* ehvi_ms, int64_t* calls,
 bo_status bo_measure_peak(int32_t what, int64_t iters, double* rate, void* stream);
 
 /*
- * Served outputs: log probabilities, routing and dispatch.
+ * Served outputs: log probabilities, routing and dispatch; expert rows and
+ * embeddings.
  *
  * Paper: the threshold router (a query's score decides which model answers
  * it), the load fractions that replace the thresholds in the search (S1), GPU
@@ -523,7 +528,7 @@ bo_status bo_measure_peak(int32_t what, int64_t iters, double* rate, void* strea
  * probabilities, the router sends each query (or each token of an expert
  * model) to its best models, and the choices are grouped by model.
  *
- * These calls take logits of the type that the model gives them in. They keep
+ * These calls take values of the type that the model gives them in. They keep
  * no state, allocate nothing and may run on any number of streams at once;
  * all are asynchronous and can be captured in a graph.
  */
@@ -694,6 +699,171 @@ int64_t bo_dispatch_workspace(int64_t N, int32_t E);
 bo_status bo_dispatch(const int32_t* ids, int64_t N, int32_t E, int64_t capacity, int32_t* load,
                       int32_t* offsets, int32_t* order, int32_t* position, void* workspace,
                       int64_t workspace_bytes, void* stream);
+
+/*
+ * bo_linear_logprobs — log probability of a given token per row, entropy, and
+ * the softmax's statistics, from hidden rows and an output matrix. The logits
+ *   l_tj = sum_h hidden_th weight_jh
+ * are formed in tiles and never stored; products of 16-bit values are exact,
+ * sums are held in fp32. All else is bo_token_logprobs' on these logits, its
+ * special values included: with x_j = inv_temperature l_j, m = max_j l_j and
+ * s = sum_j exp(inv_temperature (l_j - m)):
+ *   logprob = x_t - lse, entropy, stats = (m, log s)
+ * (the cross entropy of a row is -logprob). A token < 0 stands for none:
+ * logprob 0; a token >= V gives logprob NaN. A NaN or +inf logit makes the
+ * row's results NaN. The order of summation is fixed: a call repeats bit for
+ * bit; rows may differ in the last bits between calls of other sizes.
+ *
+ * hidden   device [T][hidden_stride] of `type`, the first H of each row used
+ * weight   device [V][weight_stride] of `type`, likewise
+ *          both aligned to their type, strides >= H (any when one row)
+ * tokens   device int64 [T], or NULL: no row has a token
+ * inv_temperature  in (0, 1e30]
+ * logprob, entropy device [T] out; stats device [T][2] out
+ * workspace  device, aligned to 16 bytes, of at least
+ *          bo_linear_logprobs_workspace(..) bytes for these matrices;
+ *          overwritten; calls that may overlap need one each. Rows that are
+ *          not aligned to 4 bytes are copied into it first.
+ * T >= 0 (0 is a no-op), T < 2^31, 1 <= V <= 2^30, T V <= 2^38,
+ * 1 <= H <= BO_MAX_WIDTH.
+ * Asynchronous. Errors: INVALID_ARGUMENT, CAPACITY, DEVICE.
+ */
+#define BO_MAX_WIDTH (1 << 20)   /* elements of a hidden row                */
+int64_t bo_linear_logprobs_workspace(const void* hidden, int64_t hidden_stride, const void* weight,
+                                     int64_t weight_stride, int32_t type, int64_t T, int64_t V,
+                                     int64_t H);
+bo_status bo_linear_logprobs(const void* hidden, int64_t hidden_stride, const void* weight,
+                             int64_t weight_stride, int32_t type, int64_t T, int64_t V, int64_t H,
+                             const int64_t* tokens, float inv_temperature, float* logprob,
+                             float* entropy, float* stats, void* workspace,
+                             int64_t workspace_bytes, void* stream);
+
+/*
+ * bo_linear_logprobs_grad — the gradients of hidden rows and output matrix from
+ * those of the log probability and the entropy.
+ *
+ * With u_j = x_j - lse, p_j = exp(u_j):
+ *   d_tj = inv_temperature ( g_t 1[j = t] - p_j (g_t + g_H (u_j + entropy)) )
+ *   grad_hidden_t = sum_j d_tj weight_j,   grad_weight_j = sum_t d_tj hidden_t
+ * g_t counts as 0 in a row without a token. A row whose g_t and g_H are both 0
+ * has gradient 0 and adds nothing to the matrix's, whatever it holds; any other
+ * row with NaN stats, or a token >= V, makes its own gradient and the matrix's
+ * NaN.
+ *
+ * The logits are formed again, in pieces of the vocabulary. For 16-bit types a
+ * piece of d is held in that type (f16: scaled by a power of two for the whole
+ * call, so that its largest is near 2^14): one rounding of each d, which is of
+ * the size of the outputs' own; sums are fp32, and the outputs rounded once.
+ *
+ * stats, entropy: as bo_linear_logprobs returned them
+ * grad_logprob, grad_entropy device [T], or NULL: 0
+ * grad_hidden device [T][grad_hidden_stride] of `type` out, or NULL: not wanted
+ * grad_weight device [V][grad_weight_stride] of `type` out, or NULL: not wanted
+ *          (neither may overlap an input or the other; T = 0 clears grad_weight)
+ * workspace  as above, of bo_linear_logprobs_grad_workspace(..) bytes
+ * Other arguments and limits as bo_linear_logprobs.
+ * Asynchronous. Errors: INVALID_ARGUMENT, CAPACITY, DEVICE.
+ */
+int64_t bo_linear_logprobs_grad_workspace(const void* hidden, int64_t hidden_stride,
+                                          const void* weight, int64_t weight_stride, int32_t type,
+                                          int64_t T, int64_t V, int64_t H);
+bo_status bo_linear_logprobs_grad(const void* hidden, int64_t hidden_stride, const void* weight,
+                                  int64_t weight_stride, int32_t type, int64_t T, int64_t V,
+                                  int64_t H, const int64_t* tokens, float inv_temperature,
+                                  const float* stats, const float* entropy,
+                                  const float* grad_logprob, const float* grad_entropy,
+                                  void* grad_hidden, int64_t grad_hidden_stride, void* grad_weight,
+                                  int64_t grad_weight_stride, void* workspace,
+                                  int64_t workspace_bytes, void* stream);
+
+/*
+ * bo_expert_gather — tokens into rows grouped by expert, as bo_dispatch placed
+ * them: row position[t,k] = x[t] for each pair; rows i with order[i] < 0 are 0.
+ * Its gradient is bo_expert_combine without weights.
+ *
+ * x        device [T][stride] of `type`, the first H of each row used
+ * order    device int32 [R], position device int32 [T][top]: bo_dispatch's for
+ *          ids [T][top]; R rows are kept (the first R of order; R <= T top,
+ *          T top when all are). A position outside [0, R) stands for none; the
+ *          others are distinct, and order[position[p]] = p.
+ * out      device [R][out_stride] of `type` out; outputs of these calls may
+ *          not overlap their inputs
+ * top      1..BO_MAX_CHOICES; H >= 1; T top < 2^31 - 65536
+ * Asynchronous. Errors: INVALID_ARGUMENT, CAPACITY, DEVICE.
+ */
+bo_status bo_expert_gather(const void* x, int32_t type, int64_t T, int64_t H, int64_t stride,
+                           int32_t top, const int32_t* order, int64_t R, const int32_t* position,
+                           void* out, int64_t out_stride, void* stream);
+
+/*
+ * bo_expert_combine — the experts' rows back to their tokens:
+ *   out[t] = sum_k weights[t,k] rows[position[t,k]]
+ * in fp32, k rising, rounded once; pairs without a row are left out (a token
+ * with none: 0), and rows that no pair has are not read.
+ *
+ * rows     device [R][stride] of `type`
+ * position device int32 [T][top]; outside [0, R): none
+ * weights  device [T][top], or NULL: 1
+ * out      device [T][out_stride] of `type` out
+ * Limits as bo_expert_gather. Asynchronous.
+ * Errors: INVALID_ARGUMENT, CAPACITY, DEVICE.
+ */
+bo_status bo_expert_combine(const void* rows, int32_t type, int64_t R, int64_t H, int64_t stride,
+                            const int32_t* position, int64_t T, int32_t top, const float* weights,
+                            void* out, int64_t out_stride, void* stream);
+
+/*
+ * bo_expert_combine_grad — the gradients of the experts' rows and of the weights:
+ *   grad_rows[position[t,k]] = weights[t,k] grad[t]   (rows i with order[i] < 0: 0)
+ *   grad_weights[t,k] = sum_h grad[t,h] rows[position[t,k],h]   (no row: 0)
+ *
+ * grad     device [T][grad_stride] of `type`: the gradient of bo_expert_combine's out
+ * rows, order, position, weights: as above
+ * grad_rows device [R][grad_rows_stride] of `type` out, rounded once, or NULL:
+ *          not wanted; grad_weights device [T][top] out, or NULL. rows is not
+ *          read (and may be NULL) where grad_weights is NULL
+ * Limits as bo_expert_gather. Asynchronous.
+ * Errors: INVALID_ARGUMENT, CAPACITY, DEVICE.
+ */
+bo_status bo_expert_combine_grad(const void* grad, int32_t type, int64_t T, int64_t H,
+                                 int64_t grad_stride, const void* rows, int64_t R, int64_t stride,
+                                 int32_t top, const int32_t* order, const int32_t* position,
+                                 const float* weights, void* grad_rows, int64_t grad_rows_stride,
+                                 float* grad_weights, void* stream);
+
+/*
+ * bo_embed — out[t] = scale table[tokens[t]], in fp32, rounded once. A token < 0
+ * stands for none: a row of 0; a token >= V gives a row of NaN.
+ *
+ * tokens device int64 [T]; table device [V][stride] of `type`, the first H of
+ * each row used; out device [T][out_stride] of `type` out, may not overlap table
+ * 1 <= V < 2^31, H >= 1, 0 <= T < 2^31 - 65536; scale finite
+ * Asynchronous. Errors: INVALID_ARGUMENT, CAPACITY, DEVICE.
+ */
+bo_status bo_embed(const int64_t* tokens, int64_t T, const void* table, int32_t type, int64_t V,
+                   int64_t H, int64_t stride, float scale, void* out, int64_t out_stride,
+                   void* stream);
+
+/*
+ * bo_embed_grad — the gradient of the table:
+ *   grad_table[v] = scale sum over t with tokens[t] = v of grad[t]
+ * in fp32 and in an order that tokens alone decide (a call repeats bit for bit),
+ * rounded once; rows without a token are 0. Tokens outside [0, V) add nothing,
+ * and their rows of grad are not read.
+ *
+ * grad device [T][stride] of `type`; grad_table device [V][grad_table_stride] of
+ * `type` out, may not overlap grad
+ * workspace  device, aligned to 16 bytes, of bo_embed_grad_workspace(T, V, H)
+ *        bytes (NULL when that is 0); overwritten; calls that may overlap need
+ *        one each
+ * Other arguments and limits as bo_embed. Asynchronous.
+ * Errors: INVALID_ARGUMENT, CAPACITY, DEVICE.
+ */
+int64_t bo_embed_grad_workspace(int64_t T, int64_t V, int64_t H);
+bo_status bo_embed_grad(const int64_t* tokens, int64_t T, const void* grad, int32_t type, int64_t H,
+                        int64_t stride, float scale, int64_t V, void* grad_table,
+                        int64_t grad_table_stride, void* workspace, int64_t workspace_bytes,
+                        void* stream);
 
 /* Releases a model (waits for its last stream first). NULL is a no-op. */
 void bo_free(bo_model model);

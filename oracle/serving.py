@@ -1,5 +1,6 @@
 """fp64 references of the served-output operators: log probabilities of given
-tokens, routing to experts, and the grouping of choices by expert.
+tokens (from logits, or from hidden rows and an output matrix), routing to
+experts, the grouping of choices by expert, the experts' rows, and embeddings.
 
 Written row by row from the definitions; logits come in whatever precision the
 caller has and are taken at their exact values. -inf masks a logit; a row whose
@@ -219,3 +220,89 @@ def dispatch(ids, experts, capacity=0):
     order[:len(kept)] = kept
     position[kept] = np.arange(len(kept))
     return dict(load=load, offsets=offsets, order=order, position=position.reshape(np.shape(ids)))
+
+
+def linear_logprobs(hidden, weight, tokens, inv_temperature=1.0):
+    """token_logprobs' dict for the logits hidden weight^T, which it holds too."""
+    logits = np.asarray(hidden, dtype=np.float64) @ np.asarray(weight, dtype=np.float64).T
+    return dict(token_logprobs(logits, tokens, 0, inv_temperature), logits=logits)
+
+
+def linear_logprobs_grad(hidden, weight, tokens, g_logprob=None, g_entropy=None, inv_temperature=1.0):
+    """(gradient of hidden, of weight, of the logits) of sum(g_logprob logprob +
+    g_entropy entropy): a row whose incoming gradients are both 0 takes no part."""
+    h, w = np.asarray(hidden, dtype=np.float64), np.asarray(weight, dtype=np.float64)
+    T, V = h.shape[0], w.shape[0]
+    tok = np.full(T, -1) if tokens is None else np.asarray(tokens)
+    gl = np.zeros(T) if g_logprob is None else np.where(tok >= 0, np.asarray(g_logprob, dtype=np.float64), 0.0)
+    gh = np.zeros(T) if g_entropy is None else np.asarray(g_entropy, dtype=np.float64)
+    live = (gl != 0) | (gh != 0)
+    d = np.zeros((T, V))
+    d[live] = token_logprobs_grad(h[live] @ w.T, tok[live], gl[live], gh[live],
+                                  inv_temperature=inv_temperature)
+    grad_h = np.zeros_like(h)
+    grad_h[live] = d[live] @ w
+    return grad_h, d[live].T @ h[live], d
+
+
+def expert_gather(x, order, top):
+    x = np.asarray(x, dtype=np.float64)
+    out = np.zeros((len(order), x.shape[1]))
+    for i, p in enumerate(order):
+        if p >= 0:
+            out[i] = x[p // top]
+    return out
+
+
+def expert_combine(rows, position, weights=None):
+    """(sum, sum of the terms' sizes)."""
+    rows, position = np.asarray(rows, dtype=np.float64), np.asarray(position)
+    T, top = position.shape
+    out, size = np.zeros((T, rows.shape[1])), np.zeros((T, rows.shape[1]))
+    for t in range(T):
+        for k in range(top):
+            i = position[t, k]
+            if 0 <= i < len(rows):
+                term = rows[i] * (1.0 if weights is None else float(weights[t, k]))
+                out[t] += term
+                size[t] += np.abs(term)
+    return out, size
+
+
+def expert_combine_grad(grad, rows, order, position, weights=None):
+    """(gradient of rows, of weights, sizes of the terms of the latter)."""
+    grad, rows = np.asarray(grad, dtype=np.float64), np.asarray(rows, dtype=np.float64)
+    T, top = np.shape(position)
+    g_rows, g_w, size = np.zeros_like(rows), np.zeros((T, top)), np.zeros((T, top))
+    for i, p in enumerate(order):
+        if p >= 0:
+            g_rows[i] = grad[p // top] * (1.0 if weights is None else float(weights[p // top, p % top]))
+    for t in range(T):
+        for k in range(top):
+            i = position[t, k]
+            if 0 <= i < len(rows):
+                g_w[t, k] = grad[t] @ rows[i]
+                size[t, k] = np.abs(grad[t]) @ np.abs(rows[i])
+    return g_rows, g_w, size
+
+
+def embed(tokens, table, scale=1.0):
+    table = np.asarray(table, dtype=np.float64)
+    out = np.zeros((len(tokens), table.shape[1]))
+    for t, v in enumerate(tokens):
+        if v >= 0:
+            out[t] = float(np.float32(scale)) * table[v] if v < len(table) else np.nan
+    return out
+
+
+def embed_grad(tokens, grad, vocab, scale=1.0):
+    """(gradient of the table, sums of the terms' sizes, tokens per row)."""
+    grad = np.asarray(grad, dtype=np.float64)
+    out, size, count = np.zeros((vocab, grad.shape[1])), np.zeros((vocab, grad.shape[1])), np.zeros(vocab, int)
+    s = float(np.float32(scale))
+    for t, v in enumerate(tokens):
+        if 0 <= v < vocab:
+            out[v] += s * grad[t]
+            size[v] += np.abs(s * grad[t])
+            count[v] += 1
+    return out, size, count

@@ -11,7 +11,9 @@ Functions mirror the C ABI in ``include/bo.h``:
 thresholds are given), ``nehvi_prepare`` / ``score_nehvi`` / ``Model.nehvi_front``
 (``bo_nehvi_prepare``, ``bo_score_nehvi``, ``bo_nehvi_front``), ``argmax``,
 ``cholesky_test`` (device), ``token_logprobs`` / ``token_logprobs_grad``, ``route``
-/ ``route_grad`` and ``dispatch`` (``bo_token_logprobs`` and so on) and
+/ ``route_grad``, ``dispatch``, ``linear_logprobs`` / ``linear_logprobs_grad``,
+``expert_gather`` / ``expert_combine`` / ``expert_combine_grad`` and ``embed`` /
+``embed_grad`` (``bo_token_logprobs`` and so on) and
 ``pareto_front``, ``box_decomposition`` (host geometry, no GPU needed).
 """
 from __future__ import annotations
@@ -25,7 +27,9 @@ import numpy as np
 __all__ = ["BoError", "Model", "lib", "lib_path", "fit", "fit_composite", "mll", "score", "score_noalloc", "nehvi_prepare", "score_nehvi", "argmax",
            "cholesky_test", "draw_fronts3_test", "profile_enable", "profile_read", "measure_peak", "pareto_front", "box_decomposition", "STATUS",
            "TokenLogprobs", "token_logprobs", "token_logprobs_grad", "Routing", "route", "route_grad",
-           "Dispatch", "dispatch", "MAX_ALTERNATIVES", "MAX_EXPERTS", "MAX_CHOICES",
+           "Dispatch", "dispatch", "LinearLogprobs", "LinearLogprobsGrad", "linear_logprobs",
+           "linear_logprobs_grad", "expert_gather", "expert_combine", "ExpertCombineGrad",
+           "expert_combine_grad", "embed", "embed_grad", "MAX_WIDTH", "MAX_ALTERNATIVES", "MAX_EXPERTS", "MAX_CHOICES",
            "MAX_N", "MAX_D", "MAX_S", "MAX_BOXES"]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -38,7 +42,7 @@ STATUS = {
     6: "BO_ERR_NONFINITE_INPUT", 7: "BO_ERR_ILL_CONDITIONED",
 }
 MAX_N, MAX_D, MAX_S, MAX_BOXES = 2048, 32, 4096, 4096
-MAX_ALTERNATIVES, MAX_EXPERTS, MAX_CHOICES = 64, 1024, 32
+MAX_ALTERNATIVES, MAX_EXPERTS, MAX_CHOICES, MAX_WIDTH = 64, 1024, 32, 1 << 20
 
 
 class BoError(RuntimeError):
@@ -123,6 +127,29 @@ def lib() -> ctypes.CDLL:
     L.bo_dispatch_workspace.restype = i64
     L.bo_dispatch.argtypes = [vp, i64, i32, i64, vp, vp, vp, vp, vp, i64, vp]
     L.bo_dispatch.restype = ctypes.c_int
+    L.bo_linear_logprobs_workspace.argtypes = [vp, i64, vp, i64, i32, i64, i64, i64]
+    L.bo_linear_logprobs_workspace.restype = i64
+    L.bo_linear_logprobs.argtypes = [vp, i64, vp, i64, i32, i64, i64, i64, vp, f32, vp, vp, vp, vp,
+                                     i64, vp]
+    L.bo_linear_logprobs.restype = ctypes.c_int
+    L.bo_linear_logprobs_grad_workspace.argtypes = L.bo_linear_logprobs_workspace.argtypes
+    L.bo_linear_logprobs_grad_workspace.restype = i64
+    L.bo_linear_logprobs_grad.argtypes = [vp, i64, vp, i64, i32, i64, i64, i64, vp, f32, vp, vp, vp,
+                                          vp, vp, i64, vp, i64, vp, i64, vp]
+    L.bo_linear_logprobs_grad.restype = ctypes.c_int
+    L.bo_expert_gather.argtypes = [vp, i32, i64, i64, i64, i32, vp, i64, vp, vp, i64, vp]
+    L.bo_expert_gather.restype = ctypes.c_int
+    L.bo_expert_combine.argtypes = [vp, i32, i64, i64, i64, vp, i64, i32, vp, vp, i64, vp]
+    L.bo_expert_combine.restype = ctypes.c_int
+    L.bo_expert_combine_grad.argtypes = [vp, i32, i64, i64, i64, vp, i64, i64, i32, vp, vp, vp, vp,
+                                         i64, vp, vp]
+    L.bo_expert_combine_grad.restype = ctypes.c_int
+    L.bo_embed.argtypes = [vp, i64, vp, i32, i64, i64, i64, f32, vp, i64, vp]
+    L.bo_embed.restype = ctypes.c_int
+    L.bo_embed_grad_workspace.argtypes = [i64, i64, i64]
+    L.bo_embed_grad_workspace.restype = i64
+    L.bo_embed_grad.argtypes = [vp, i64, vp, i32, i64, i64, f32, i64, vp, i64, vp, i64, vp]
+    L.bo_embed_grad.restype = ctypes.c_int
     L.bo_free.argtypes = [vp]
     L.bo_free.restype = None
     L.bo_status_string.argtypes = [ctypes.c_int]
@@ -675,6 +702,222 @@ def dispatch(ids, experts, capacity=0, out=None, stream=None):
     st = L.bo_dispatch(idp, N, E, capacity, *ptrs, wp, need, _stream_of(ids, stream))
     if st:
         _check(st, "bo_dispatch")
+    return out
+
+
+class LinearLogprobs(NamedTuple):
+    """What linear_logprobs returns, row by row: fp32 ``logprob`` (minus the
+    cross entropy), ``entropy`` and ``stats`` [T, 2] (largest logit, log of the
+    sum relative to it)."""
+    logprob: object
+    entropy: object
+    stats: object
+
+
+class LinearLogprobsGrad(NamedTuple):
+    """Gradients of linear_logprobs' ``hidden`` and ``weight`` (None where not
+    asked for)."""
+    hidden: object
+    weight: object
+
+
+class ExpertCombineGrad(NamedTuple):
+    """Gradients of expert_combine's ``rows`` and ``weights`` (None where not
+    asked for)."""
+    rows: object
+    weights: object
+
+
+def _pair(hidden, weight):
+    """The arguments that describe hidden rows and output matrix, and T, V, H."""
+    hp, kind, T, H, hs = _rows(hidden, "hidden")
+    wp, wkind, V, wH, ws = _rows(weight, "weight")
+    if wkind != kind or wH != H:
+        raise ValueError("hidden and weight must have the same type and columns")
+    return (hp, hs, wp, ws, kind, T, V, H), T, V, H
+
+
+def linear_logprobs(hidden, weight, tokens=None, inv_temperature=1.0, out=None, stream=None):
+    """bo_linear_logprobs: token_logprobs' log probability and entropy for the
+    logits ``hidden @ weight.T`` (hidden [T, H], weight [V, H], both fp32, bf16 or
+    fp16 GPU tensors, rows any distance apart), which are not stored. tokens
+    int64 [T] (negative: none) or None. Returns a LinearLogprobs; ``out`` takes
+    one of the same shapes to write into. Outside autograd: the gradients are
+    linear_logprobs_grad's."""
+    args, T, V, H = _pair(hidden, weight)
+    tp = None if tokens is None else _vec(tokens, "tokens", _i64, (T,))
+    specs = (((T,), _f32), ((T,), _f32), ((T, 2), _f32))
+    if out is None:
+        out = LinearLogprobs(*_new(hidden, stream, *specs))
+        ptrs = [t.data_ptr() for t in out]
+    else:
+        ptrs = [_vec(t, n, d, s) for t, n, (s, d) in zip(out, LinearLogprobs._fields, specs)]
+    L = _lib or lib()
+    need = L.bo_linear_logprobs_workspace(*args)
+    ws, wp = _workspace(hidden, stream, need)
+    st = L.bo_linear_logprobs(*args, tp, inv_temperature, *ptrs, wp, need, _stream_of(hidden, stream))
+    if st:
+        _check(st, "bo_linear_logprobs")
+    return out
+
+
+def linear_logprobs_grad(hidden, weight, tokens, stats, entropy, grad_logprob=None,
+                         grad_entropy=None, inv_temperature=1.0, want=(True, True), out=None,
+                         stream=None):
+    """bo_linear_logprobs_grad: the gradients of hidden and weight (their shapes
+    and type) from those of linear_logprobs' outputs; ``stats`` and ``entropy`` as
+    it returned them. ``want`` says which of the two are formed; the other is
+    None. Returns a LinearLogprobsGrad; ``out`` takes one to write into (its
+    tensors then say what is wanted)."""
+    args, T, V, H = _pair(hidden, weight)
+    tp = None if tokens is None else _vec(tokens, "tokens", _i64, (T,))
+    sp, ep = _vec(stats, "stats", _f32, (T, 2)), _vec(entropy, "entropy", _f32, (T,))
+    gl = None if grad_logprob is None else _vec(grad_logprob, "grad_logprob", _f32, (T,))
+    gh = None if grad_entropy is None else _vec(grad_entropy, "grad_entropy", _f32, (T,))
+    if out is None:
+        out = LinearLogprobsGrad(*(_new(hidden, stream, (shape, hidden.dtype))[0] if on else None
+                                   for on, shape in zip(want, ((T, H), (V, H)))))
+    op = [None, 0, None, 0]
+    for i, (t, rows, name) in enumerate(zip(out, (T, V), ("hidden", "weight"))):
+        if t is not None:
+            p, okind, oT, oH, ostride = _rows(t, "out")
+            if (okind, oT, oH) != (args[4], rows, H):
+                raise ValueError(f"out.{name} must have the shape and type of {name}")
+            op[2 * i:2 * i + 2] = p, ostride
+    L = _lib or lib()
+    need = L.bo_linear_logprobs_grad_workspace(*args)
+    ws, wp = _workspace(hidden, stream, need)
+    st = L.bo_linear_logprobs_grad(*args, tp, inv_temperature, sp, ep, gl, gh, *op, wp, need,
+                                   _stream_of(hidden, stream))
+    if st:
+        _check(st, "bo_linear_logprobs_grad")
+    return out
+
+
+def _places(order, position, rows=None):
+    """(order's pointer or None, position's, T, top, R); R from order or rows."""
+    if _TYPES is None:
+        _torch_types()
+    if getattr(position, "ndim", 0) != 2:
+        raise TypeError("position must be an int32 matrix on the GPU")
+    T, top = position.shape
+    pp = _vec(position, "position", _i32, (T, top))
+    if order is None:
+        return None, pp, T, top, rows
+    if getattr(order, "ndim", 0) != 1:
+        raise TypeError("order must be an int32 vector on the GPU")
+    R = order.shape[0]
+    return _vec(order, "order", _i32, (R,)), pp, T, top, R
+
+
+def _out_rows(out, like, kind, stream, R, H):
+    if out is None:
+        out, = _new(like, stream, ((R, H), like.dtype))
+    op, okind, oR, oH, ostride = _rows(out, "out")
+    if (okind, oR, oH) != (kind, R, H):
+        raise ValueError(f"out must have shape {(R, H)} and the input's type")
+    return out, op, ostride
+
+
+def expert_gather(x, order, position, out=None, stream=None):
+    """bo_expert_gather: the tokens x [T, H] (fp32, bf16 or fp16 GPU tensor, rows
+    any distance apart) in rows grouped by expert [R, H], as dispatch placed them:
+    ``order`` (its first R entries, all or, with a capacity, as many as can be
+    kept) and ``position`` [T, top]. Rows that no pair fills are 0. Outside
+    autograd: the gradient of x is expert_combine of the rows' gradient, without
+    weights."""
+    xp, kind, T, H, stride = _rows(x, "x")
+    ip, pp, pT, top, R = _places(order, position)
+    if pT != T:
+        raise ValueError("position must have a row per token")
+    out, op, ostride = _out_rows(out, x, kind, stream, R, H)
+    st = (_lib or lib()).bo_expert_gather(xp, kind, T, H, stride, top, ip, R, pp, op, ostride,
+                                          _stream_of(x, stream))
+    if st:
+        _check(st, "bo_expert_gather")
+    return out
+
+
+def expert_combine(rows, position, weights=None, out=None, stream=None):
+    """bo_expert_combine: the experts' rows [R, H] (fp32, bf16 or fp16 GPU tensor,
+    rows any distance apart) back to their tokens [T, H], summed under the
+    router's ``weights`` fp32 [T, top] (None: 1). Pairs without a row are left
+    out. Outside autograd: the gradients are expert_combine_grad's."""
+    rp, kind, R, H, stride = _rows(rows, "rows")
+    _, pp, T, top, _ = _places(None, position)
+    wp = None if weights is None else _vec(weights, "weights", _f32, (T, top))
+    out, op, ostride = _out_rows(out, rows, kind, stream, T, H)
+    st = (_lib or lib()).bo_expert_combine(rp, kind, R, H, stride, pp, T, top, wp, op, ostride,
+                                           _stream_of(rows, stream))
+    if st:
+        _check(st, "bo_expert_combine")
+    return out
+
+
+def expert_combine_grad(grad, rows, order, position, weights=None, want=(True, True), out=None,
+                        stream=None):
+    """bo_expert_combine_grad: the gradients of expert_combine's rows ([R, H],
+    their type) and weights (fp32 [T, top]) from that of its output, ``grad``
+    [T, H]. ``want`` says which of the two are formed; the other is None. Returns
+    an ExpertCombineGrad; ``out`` takes one to write into (its tensors then say
+    what is wanted)."""
+    gp, kind, T, H, gstride = _rows(grad, "grad")
+    rp, rkind, R, rH, stride = _rows(rows, "rows")
+    if (rkind, rH) != (kind, H):
+        raise ValueError("grad and rows must have the same type and columns")
+    ip, pp, pT, top, oR = _places(order, position)
+    if pT != T or oR != R:
+        raise ValueError("position must have a row per token, order an entry per row")
+    wp = None if weights is None else _vec(weights, "weights", _f32, (T, top))
+    if out is None:
+        out = ExpertCombineGrad(
+            _new(grad, stream, ((R, H), grad.dtype))[0] if want[0] else None,
+            _new(grad, stream, ((T, top), _f32))[0] if want[1] else None)
+    op, ostride = None, 0
+    if out[0] is not None:
+        _, op, ostride = _out_rows(out[0], grad, kind, stream, R, H)
+    gwp = None if out[1] is None else _vec(out[1], "weights", _f32, (T, top))
+    st = (_lib or lib()).bo_expert_combine_grad(gp, kind, T, H, gstride, rp, R, stride, top, ip, pp,
+                                                wp, op, ostride, gwp, _stream_of(grad, stream))
+    if st:
+        _check(st, "bo_expert_combine_grad")
+    return out
+
+
+def embed(tokens, table, scale=1.0, out=None, stream=None):
+    """bo_embed: ``scale`` times the rows of table [V, H] (fp32, bf16 or fp16 GPU
+    tensor, rows any distance apart) that the tokens (int64 GPU tensor [T])
+    name, [T, H]; a row of 0 for a negative token. Outside autograd: the table's
+    gradient is embed_grad's."""
+    tp_, kind, V, H, stride = _rows(table, "table")
+    if getattr(tokens, "ndim", 0) != 1:
+        raise TypeError("tokens must be an int64 vector on the GPU")
+    T = tokens.shape[0]
+    ip = _vec(tokens, "tokens", _i64, (T,))
+    out, op, ostride = _out_rows(out, table, kind, stream, T, H)
+    st = (_lib or lib()).bo_embed(ip, T, tp_, kind, V, H, stride, scale, op, ostride,
+                                  _stream_of(table, stream))
+    if st:
+        _check(st, "bo_embed")
+    return out
+
+
+def embed_grad(tokens, grad, vocab, scale=1.0, out=None, stream=None):
+    """bo_embed_grad: the gradient of embed's table ([vocab, H], the type of
+    ``grad``) from that of its rows, ``grad`` [T, H]."""
+    gp, kind, T, H, stride = _rows(grad, "grad")
+    ip = _vec(tokens, "tokens", _i64, (T,))
+    V = int(vocab)
+    if V < 1:
+        raise ValueError("vocab must be at least 1")
+    out, op, ostride = _out_rows(out, grad, kind, stream, V, H)
+    L = _lib or lib()
+    need = L.bo_embed_grad_workspace(T, V, H)
+    ws, wp = _workspace(grad, stream, need)
+    st = L.bo_embed_grad(ip, T, gp, kind, H, stride, scale, V, op, ostride, wp, need,
+                         _stream_of(grad, stream))
+    if st:
+        _check(st, "bo_embed_grad")
     return out
 
 

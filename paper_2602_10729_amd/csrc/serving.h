@@ -1,5 +1,6 @@
 // Internal declarations of the served-output operators: log probabilities
-// (logprobs.hip), routing (route.hip) and dispatch (dispatch.hip).
+// (logprobs.hip; from hidden rows linear.hip), routing (route.hip), dispatch
+// (dispatch.hip), expert rows (experts.hip) and embeddings (embed.hip).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -246,5 +247,63 @@ int64_t dispatch_workspace(int64_t N, int E);
 hipError_t launch_dispatch(const int32_t* ids, int64_t N, int E, int64_t capacity, int32_t* load,
                            int32_t* offsets, int32_t* order, int32_t* position, void* ws,
                            hipStream_t st);
+
+struct ExpertArgs {
+  const void* tokens;          // [T][H]: the layer's inputs, or the gradient of its outputs
+  const void* rows;            // [R][H]: the experts' outputs
+  int type;
+  int64_t T, H, R;
+  int64_t stride, rows_stride;
+  int top;
+  const int32_t* order;
+  const int32_t* position;
+  const float* weights;        // or nullptr: 1
+  void* out;                   // or nullptr (gradient)
+  int64_t out_stride;
+  float* grad_weights;         // or nullptr
+};
+hipError_t launch_expert_gather(const ExpertArgs& a, hipStream_t st);
+hipError_t launch_expert_combine(const ExpertArgs& a, hipStream_t st);
+hipError_t launch_expert_combine_grad(const ExpertArgs& a, hipStream_t st);
+
+struct EmbedArgs {
+  const int64_t* tokens;
+  const void* in;              // the table, or the gradient of its rows
+  int type;
+  int64_t T, V, H, stride;
+  float scale;
+  void* out;
+  int64_t out_stride;
+  void* ws;
+};
+hipError_t launch_embed(const EmbedArgs& a, hipStream_t st);
+int64_t embed_grad_workspace(int64_t T, int64_t V, int64_t H);
+hipError_t launch_embed_grad(const EmbedArgs& a, hipStream_t st);
+
+struct LinearArgs {
+  const void* hidden;
+  const void* weight;
+  int64_t hidden_stride, weight_stride;
+  int type;
+  int64_t T, V, H;
+  const int64_t* tokens;       // or nullptr
+  float it;
+  float* logprob;
+  float* entropy;
+  float* stats;
+  const float* stats_in;       // gradient
+  const float* entropy_in;
+  const float* g_logprob;      // or nullptr
+  const float* g_entropy;      // or nullptr
+  void* grad_hidden;           // or nullptr
+  int64_t grad_hidden_stride;
+  void* grad_weight;           // or nullptr
+  int64_t grad_weight_stride;
+  void* ws;
+};
+int64_t linear_workspace(const LinearArgs& a);
+hipError_t launch_linear(const LinearArgs& a, hipStream_t st);
+int64_t linear_grad_workspace(const LinearArgs& a);
+hipError_t launch_linear_grad(const LinearArgs& a, hipStream_t st);
 
 }  // namespace bo

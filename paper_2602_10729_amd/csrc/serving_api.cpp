@@ -102,6 +102,73 @@ bo_status check_route_sizes(int32_t type, int64_t T, int32_t E, int32_t score, i
   return BO_OK;
 }
 
+// Whether two matrices of `type` share an element. Rows that alternate within
+// one stride (column ranges of one buffer) do not.
+bool overlap(const void* p, int64_t p_rows, int64_t p_stride, const void* q, int64_t q_rows,
+             int64_t q_stride, int64_t cols, int32_t type) {
+  if (!p || !q || p_rows == 0 || q_rows == 0) return false;
+  const int64_t es = static_cast<int64_t>(bo::type_bytes(type));
+  uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+  const uintptr_t ae = a + static_cast<uintptr_t>(span_bytes(p_rows, cols, p_stride, es));
+  const uintptr_t be = b + static_cast<uintptr_t>(span_bytes(q_rows, cols, q_stride, es));
+  if (a >= be || b >= ae) return false;
+  if (p_stride != q_stride || p_rows == 1 || q_rows == 1) return true;
+  const uintptr_t pitch = static_cast<uintptr_t>(p_stride * es), width = static_cast<uintptr_t>(cols * es);
+  const uintptr_t off = (a > b ? a - b : b - a) % pitch;
+  return off < width || pitch - off < width;
+}
+bo_status no_overlap(bool bad, const char* where, const char* what) {
+  return bad ? fail(BO_ERR_INVALID_ARGUMENT, std::string(where) + ": " + what) : BO_OK;
+}
+
+constexpr int64_t kMaxPairs = ((int64_t)1 << 31) - 65536;
+constexpr int64_t kMaxElems = (int64_t)1 << 31;
+constexpr int64_t kMaxScores = (int64_t)1 << 38;      // (a launch's blocks and threads)
+
+bo_status check_expert_sizes(int32_t type, int64_t T, int64_t H, int32_t top, int64_t R,
+                             const char* where) {
+  const std::string W(where);
+  if (bad_type(type)) return fail(BO_ERR_INVALID_ARGUMENT, W + ": unknown type");
+  if (T < 0 || H < 1 || top < 1) return fail(BO_ERR_INVALID_ARGUMENT, W + ": T < 0, H < 1 or top < 1");
+  if (top > BO_MAX_CHOICES) return fail(BO_ERR_CAPACITY, W + ": top beyond BO_MAX_CHOICES");
+  if (T >= kMaxPairs / top || H >= kMaxElems) return fail(BO_ERR_CAPACITY, W + ": T or H beyond limit");
+  if (R < 0 || R > T * top) return fail(BO_ERR_INVALID_ARGUMENT, W + ": R must be in [0, T top]");
+  return BO_OK;
+}
+
+bo_status check_linear_sizes(int32_t type, int64_t T, int64_t V, int64_t H, float it, const char* where) {
+  const std::string W(where);
+  if (bad_type(type)) return fail(BO_ERR_INVALID_ARGUMENT, W + ": unknown type");
+  if (T < 0 || V < 1 || H < 1) return fail(BO_ERR_INVALID_ARGUMENT, W + ": T < 0, V < 1 or H < 1");
+  if (!(it > 0.0f) || !(it <= 1e30f))
+    return fail(BO_ERR_INVALID_ARGUMENT, W + ": inv_temperature must be in (0, 1e30]");
+  if (T >= kMaxElems || V > kMaxElems / 2 || T > kMaxScores / V)
+    return fail(BO_ERR_CAPACITY, W + ": T, V or T times V beyond limit");
+  if (H > BO_MAX_WIDTH) return fail(BO_ERR_CAPACITY, W + ": H beyond BO_MAX_WIDTH");
+  return BO_OK;
+}
+
+bo::LinearArgs linear_args(const void* hidden, int64_t hidden_stride, const void* weight,
+                           int64_t weight_stride, int32_t type, int64_t T, int64_t V, int64_t H) {
+  bo::LinearArgs a{};
+  a.hidden = hidden; a.hidden_stride = hidden_stride;
+  a.weight = weight; a.weight_stride = weight_stride;
+  a.type = type;
+  a.T = T; a.V = V; a.H = H;
+  return a;
+}
+
+bo_status check_embed_sizes(int32_t type, int64_t T, int64_t V, int64_t H, float scale,
+                            const char* where) {
+  const std::string W(where);
+  if (bad_type(type)) return fail(BO_ERR_INVALID_ARGUMENT, W + ": unknown type");
+  if (T < 0 || V < 1 || H < 1) return fail(BO_ERR_INVALID_ARGUMENT, W + ": T < 0, V < 1 or H < 1");
+  if (!std::isfinite(scale)) return fail(BO_ERR_INVALID_ARGUMENT, W + ": scale is not finite");
+  if (T >= kMaxPairs || V >= kMaxElems || H >= kMaxElems)
+    return fail(BO_ERR_CAPACITY, W + ": T, V or H beyond limit");
+  return BO_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -256,6 +323,216 @@ bo_status bo_dispatch(const int32_t* ids, int64_t N, int32_t E, int64_t capacity
     return bo::after_launch(bo::launch_dispatch(ids, N, E, capacity, load, offsets, order, position,
                                                 workspace, st),
                             st, W);
+  });
+}
+
+bo_status bo_expert_gather(const void* x, int32_t type, int64_t T, int64_t H, int64_t stride,
+                           int32_t top, const int32_t* order, int64_t R, const int32_t* position,
+                           void* out, int64_t out_stride, void* stream) {
+  return guarded([&]() -> bo_status {
+    const char* W = "bo_expert_gather";
+    bo_status s = check_expert_sizes(type, T, H, top, R, W);
+    if (s != BO_OK) return s;
+    if (T == 0 || R == 0) return BO_OK;
+    if ((s = check_rows(x, type, T, H, stride, W, "x")) != BO_OK) return s;
+    if ((s = check_rows(out, type, R, H, out_stride, W, "out")) != BO_OK) return s;
+    if ((s = no_overlap(overlap(x, T, stride, out, R, out_stride, H, type), W, "out overlaps x")) != BO_OK)
+      return s;
+    if ((s = check_dev(order, 4 * static_cast<size_t>(R), "order")) != BO_OK) return s;
+    if ((s = check_dev(position, 4 * static_cast<size_t>(T) * top, "position")) != BO_OK) return s;
+    bo::ExpertArgs a{x, nullptr, type, T, H, R, stride, 0, top, order, position, nullptr, out,
+                     out_stride, nullptr};
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    return bo::after_launch(bo::launch_expert_gather(a, st), st, W);
+  });
+}
+
+bo_status bo_expert_combine(const void* rows, int32_t type, int64_t R, int64_t H, int64_t stride,
+                            const int32_t* position, int64_t T, int32_t top, const float* weights,
+                            void* out, int64_t out_stride, void* stream) {
+  return guarded([&]() -> bo_status {
+    const char* W = "bo_expert_combine";
+    bo_status s = check_expert_sizes(type, T, H, top, R, W);
+    if (s != BO_OK) return s;
+    if (T == 0) return BO_OK;
+    if (R > 0 && (s = check_rows(rows, type, R, H, stride, W, "rows")) != BO_OK) return s;
+    if ((s = check_rows(out, type, T, H, out_stride, W, "out")) != BO_OK) return s;
+    if ((s = no_overlap(overlap(rows, R, stride, out, T, out_stride, H, type), W, "out overlaps rows")) != BO_OK)
+      return s;
+    const size_t n = static_cast<size_t>(T) * top;
+    if ((s = check_dev(position, 4 * n, "position")) != BO_OK) return s;
+    if (weights && (s = check_dev(weights, 4 * n, "weights")) != BO_OK) return s;
+    bo::ExpertArgs a{nullptr, rows, type, T, H, R, 0, stride, top, nullptr, position, weights, out,
+                     out_stride, nullptr};
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    return bo::after_launch(bo::launch_expert_combine(a, st), st, W);
+  });
+}
+
+bo_status bo_expert_combine_grad(const void* grad, int32_t type, int64_t T, int64_t H,
+                                 int64_t grad_stride, const void* rows, int64_t R, int64_t stride,
+                                 int32_t top, const int32_t* order, const int32_t* position,
+                                 const float* weights, void* grad_rows, int64_t grad_rows_stride,
+                                 float* grad_weights, void* stream) {
+  return guarded([&]() -> bo_status {
+    const char* W = "bo_expert_combine_grad";
+    bo_status s = check_expert_sizes(type, T, H, top, R, W);
+    if (s != BO_OK) return s;
+    if (T == 0) return BO_OK;
+    if ((s = check_rows(grad, type, T, H, grad_stride, W, "grad")) != BO_OK) return s;
+    if (grad_weights && R > 0 && (s = check_rows(rows, type, R, H, stride, W, "rows")) != BO_OK) return s;
+    const size_t n = static_cast<size_t>(T) * top;
+    if (grad_rows && R > 0) {
+      if ((s = check_rows(grad_rows, type, R, H, grad_rows_stride, W, "grad_rows")) != BO_OK) return s;
+      if ((s = no_overlap(overlap(grad, T, grad_stride, grad_rows, R, grad_rows_stride, H, type) ||
+                          (grad_weights && overlap(rows, R, stride, grad_rows, R, grad_rows_stride, H, type)),
+                          W, "grad_rows overlaps an input")) != BO_OK)
+        return s;
+      if ((s = check_dev(order, 4 * static_cast<size_t>(R), "order")) != BO_OK) return s;
+    }
+    if ((s = check_dev(position, 4 * n, "position")) != BO_OK) return s;
+    if (weights && (s = check_dev(weights, 4 * n, "weights")) != BO_OK) return s;
+    if (grad_weights && (s = check_dev(grad_weights, 4 * n, "grad_weights")) != BO_OK) return s;
+    bo::ExpertArgs a{grad, rows, type, T, H, R, grad_stride, stride, top, order, position, weights,
+                     R > 0 ? grad_rows : nullptr, grad_rows_stride, grad_weights};
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    return bo::after_launch(bo::launch_expert_combine_grad(a, st), st, W);
+  });
+}
+
+bo_status bo_embed(const int64_t* tokens, int64_t T, const void* table, int32_t type, int64_t V,
+                   int64_t H, int64_t stride, float scale, void* out, int64_t out_stride,
+                   void* stream) {
+  return guarded([&]() -> bo_status {
+    const char* W = "bo_embed";
+    bo_status s = check_embed_sizes(type, T, V, H, scale, W);
+    if (s != BO_OK) return s;
+    if (T == 0) return BO_OK;
+    if ((s = check_dev(tokens, 8 * static_cast<size_t>(T), "tokens")) != BO_OK) return s;
+    if ((s = check_rows(table, type, V, H, stride, W, "table")) != BO_OK) return s;
+    if ((s = check_rows(out, type, T, H, out_stride, W, "out")) != BO_OK) return s;
+    if ((s = no_overlap(overlap(table, V, stride, out, T, out_stride, H, type), W, "out overlaps table")) != BO_OK)
+      return s;
+    bo::EmbedArgs a{tokens, table, type, T, V, H, stride, scale, out, out_stride, nullptr};
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    return bo::after_launch(bo::launch_embed(a, st), st, W);
+  });
+}
+
+int64_t bo_embed_grad_workspace(int64_t T, int64_t V, int64_t H) {
+  if (T < 1 || T >= kMaxPairs || V < 1 || V >= kMaxElems || H < 1 || H >= kMaxElems) return 0;
+  return bo::embed_grad_workspace(T, V, H);
+}
+
+bo_status bo_embed_grad(const int64_t* tokens, int64_t T, const void* grad, int32_t type, int64_t H,
+                        int64_t stride, float scale, int64_t V, void* grad_table,
+                        int64_t grad_table_stride, void* workspace, int64_t workspace_bytes,
+                        void* stream) {
+  return guarded([&]() -> bo_status {
+    const char* W = "bo_embed_grad";
+    bo_status s = check_embed_sizes(type, T, V, H, scale, W);
+    if (s != BO_OK) return s;
+    if ((s = check_rows(grad_table, type, V, H, grad_table_stride, W, "grad_table")) != BO_OK) return s;
+    if (T > 0) {
+      if ((s = check_dev(tokens, 8 * static_cast<size_t>(T), "tokens")) != BO_OK) return s;
+      if ((s = check_rows(grad, type, T, H, stride, W, "grad")) != BO_OK) return s;
+      if ((s = no_overlap(overlap(grad, T, stride, grad_table, V, grad_table_stride, H, type), W,
+                          "grad_table overlaps grad")) != BO_OK)
+        return s;
+      if ((s = check_workspace(workspace, workspace_bytes, bo::embed_grad_workspace(T, V, H), W)) != BO_OK)
+        return s;
+    }
+    bo::EmbedArgs a{tokens, grad, type, T, V, H, stride, scale, grad_table, grad_table_stride, workspace};
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    return bo::after_launch(bo::launch_embed_grad(a, st), st, W);
+  });
+}
+
+int64_t bo_linear_logprobs_workspace(const void* hidden, int64_t hidden_stride, const void* weight,
+                                     int64_t weight_stride, int32_t type, int64_t T, int64_t V,
+                                     int64_t H) {
+  if (T == 0 || check_linear_sizes(type, T, V, H, 1.0f, "bo_linear_logprobs_workspace") != BO_OK) return 0;
+  return bo::linear_workspace(linear_args(hidden, hidden_stride, weight, weight_stride, type, T, V, H));
+}
+
+bo_status bo_linear_logprobs(const void* hidden, int64_t hidden_stride, const void* weight,
+                             int64_t weight_stride, int32_t type, int64_t T, int64_t V, int64_t H,
+                             const int64_t* tokens, float inv_temperature, float* logprob,
+                             float* entropy, float* stats, void* workspace,
+                             int64_t workspace_bytes, void* stream) {
+  return guarded([&]() -> bo_status {
+    const char* W = "bo_linear_logprobs";
+    bo_status s = check_linear_sizes(type, T, V, H, inv_temperature, W);
+    if (s != BO_OK) return s;
+    if (T == 0) return BO_OK;
+    if ((s = check_rows(hidden, type, T, H, hidden_stride, W, "hidden")) != BO_OK) return s;
+    if ((s = check_rows(weight, type, V, H, weight_stride, W, "weight")) != BO_OK) return s;
+    const size_t n = static_cast<size_t>(T);
+    if (tokens && (s = check_dev(tokens, 8 * n, "tokens")) != BO_OK) return s;
+    if ((s = check_dev(logprob, 4 * n, "logprob")) != BO_OK) return s;
+    if ((s = check_dev(entropy, 4 * n, "entropy")) != BO_OK) return s;
+    if ((s = check_dev(stats, 8 * n, "stats")) != BO_OK) return s;
+    bo::LinearArgs a = linear_args(hidden, hidden_stride, weight, weight_stride, type, T, V, H);
+    if ((s = check_workspace(workspace, workspace_bytes, bo::linear_workspace(a), W)) != BO_OK) return s;
+    a.tokens = tokens; a.it = inv_temperature;
+    a.logprob = logprob; a.entropy = entropy; a.stats = stats;
+    a.ws = workspace;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    return bo::after_launch(bo::launch_linear(a, st), st, W);
+  });
+}
+
+int64_t bo_linear_logprobs_grad_workspace(const void* hidden, int64_t hidden_stride,
+                                          const void* weight, int64_t weight_stride, int32_t type,
+                                          int64_t T, int64_t V, int64_t H) {
+  if (T == 0 || check_linear_sizes(type, T, V, H, 1.0f, "bo_linear_logprobs_grad_workspace") != BO_OK) return 0;
+  return bo::linear_grad_workspace(linear_args(hidden, hidden_stride, weight, weight_stride, type, T, V, H));
+}
+
+bo_status bo_linear_logprobs_grad(const void* hidden, int64_t hidden_stride, const void* weight,
+                                  int64_t weight_stride, int32_t type, int64_t T, int64_t V,
+                                  int64_t H, const int64_t* tokens, float inv_temperature,
+                                  const float* stats, const float* entropy,
+                                  const float* grad_logprob, const float* grad_entropy,
+                                  void* grad_hidden, int64_t grad_hidden_stride, void* grad_weight,
+                                  int64_t grad_weight_stride, void* workspace,
+                                  int64_t workspace_bytes, void* stream) {
+  return guarded([&]() -> bo_status {
+    const char* W = "bo_linear_logprobs_grad";
+    bo_status s = check_linear_sizes(type, T, V, H, inv_temperature, W);
+    if (s != BO_OK) return s;
+    if (grad_weight) {
+      if ((s = check_rows(grad_weight, type, V, H, grad_weight_stride, W, "grad_weight")) != BO_OK) return s;
+    }
+    bo::LinearArgs a = linear_args(hidden, hidden_stride, weight, weight_stride, type, T, V, H);
+    a.tokens = tokens; a.it = inv_temperature;
+    a.stats_in = stats; a.entropy_in = entropy;
+    a.g_logprob = grad_logprob; a.g_entropy = grad_entropy;
+    a.grad_hidden = grad_hidden; a.grad_hidden_stride = grad_hidden_stride;
+    a.grad_weight = grad_weight; a.grad_weight_stride = grad_weight_stride;
+    a.ws = workspace;
+    if (T > 0) {
+      if ((s = check_rows(hidden, type, T, H, hidden_stride, W, "hidden")) != BO_OK) return s;
+      if ((s = check_rows(weight, type, V, H, weight_stride, W, "weight")) != BO_OK) return s;
+      if (grad_hidden && (s = check_rows(grad_hidden, type, T, H, grad_hidden_stride, W, "grad_hidden")) != BO_OK)
+        return s;
+      const size_t n = static_cast<size_t>(T);
+      if (tokens && (s = check_dev(tokens, 8 * n, "tokens")) != BO_OK) return s;
+      if ((s = check_dev(stats, 8 * n, "stats")) != BO_OK) return s;
+      if ((s = check_dev(entropy, 4 * n, "entropy")) != BO_OK) return s;
+      if (grad_logprob && (s = check_dev(grad_logprob, 4 * n, "grad_logprob")) != BO_OK) return s;
+      if (grad_entropy && (s = check_dev(grad_entropy, 4 * n, "grad_entropy")) != BO_OK) return s;
+      if ((s = no_overlap(overlap(grad_hidden, T, grad_hidden_stride, hidden, T, hidden_stride, H, type) ||
+                          overlap(grad_hidden, T, grad_hidden_stride, weight, V, weight_stride, H, type) ||
+                          overlap(grad_weight, V, grad_weight_stride, hidden, T, hidden_stride, H, type) ||
+                          overlap(grad_weight, V, grad_weight_stride, weight, V, weight_stride, H, type) ||
+                          overlap(grad_hidden, T, grad_hidden_stride, grad_weight, V, grad_weight_stride, H, type),
+                          W, "a gradient overlaps an input or the other gradient")) != BO_OK)
+        return s;
+      if ((s = check_workspace(workspace, workspace_bytes, bo::linear_grad_workspace(a), W)) != BO_OK) return s;
+    }
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    return bo::after_launch(bo::launch_linear_grad(a, st), st, W);
   });
 }
 
