@@ -2,7 +2,7 @@
 // gradients of both: the plan of a call, and what happens beside the products of
 // linear_tile.h.
 //
-// Forward: one product, whose tiles leave three numbers a token and 32 to 128
+// Forward: one product, whose tiles leave three numbers a token and 128 or 256
 // logits, and a join of them. Backward: the vocabulary in pieces; a piece's d is
 // formed by the same product (the logits are not kept, so their 2 T V H
 // operations are done again: 8 T V H in all), read twice: into fp32 sums of
@@ -42,13 +42,33 @@ Shape shape_of(const LinearArgs& a) {
   return s;
 }
 
-TileShape forward_shape(int64_t T, int64_t V) {
-  if (T <= 32) return kNarrow32;
-  if (T <= 64) return kNarrow64;
-  return up(T, 256) / 256 * (up(V, 256) / 256) >= kUnits ? kBig : kMiddle;
+int64_t tiles_of(TileShape t, int64_t M, int64_t N) {
+  return up(M, tile_m(t)) / tile_m(t) * (up(N, tile_n(t)) / tile_n(t));
 }
-TileShape wide_shape(int64_t M, int64_t N) {
-  return up(M, 256) / 256 * (up(N, 256) / 256) >= kUnits ? kBig : kMiddle;
+
+// The shape of the tiles and the splits of k that should take the least time: whole
+// rounds of workgroups (one large tile a compute unit, or two of the quarter's
+// size, which take 1.2 times as long for the same work), and for split sums their
+// way through memory. In microseconds: a large k-tile takes 1.7 (16 bits) or 7.2
+// (fp32), memory 4 bytes a picosecond.
+struct Choice {
+  TileShape tile;
+  int64_t splits;
+  double cost;
+};
+Choice choose(int type, int64_t M, int64_t N, int64_t k_tiles, int64_t most_splits) {
+  Choice best{kBig, 1, 1e300};
+  for (const TileShape t : {kBig, kMiddle}) {
+    const int64_t tiles = tiles_of(t, M, N), at_once = t == kBig ? kUnits : 2 * kUnits;
+    const double k_tile = (type == BO_TYPE_F32 ? 7.2 : 1.7) * (t == kBig ? 1.0 : 0.6);
+    for (int64_t s = 1; s <= most_splits && (s == 1 || s <= k_tiles / 8); ++s) {
+      const double rounds = static_cast<double>((tiles * s + at_once - 1) / at_once);
+      const double sums = s == 1 ? 0.0 : 8e-6 * static_cast<double>(s) * static_cast<double>(M) * static_cast<double>(N) / 4.0;
+      const double cost = rounds * static_cast<double>((k_tiles + s - 1) / s) * k_tile + sums + (s > 1 ? 5.0 : 0.0);
+      if (cost < best.cost) best = {t, s, cost};
+    }
+  }
+  return best;
 }
 
 struct Forward {
@@ -58,8 +78,8 @@ struct Forward {
 };
 Forward forward_plan(const Shape& s) {
   Forward f;
-  f.tile = forward_shape(s.T, s.V);
-  f.slots = up(s.V, tile_m(f.tile)) / tile_m(f.tile) * tile_wave_rows(f.tile);
+  f.tile = s.T <= 32 ? kNarrow32 : s.T <= 64 ? kNarrow64 : choose(s.type, s.V, s.T, 1, 1).tile;
+  f.slots = up(s.V, tile_m(f.tile)) / tile_m(f.tile);
   int64_t at = 0;
   const auto take = [&](int64_t bytes) { const int64_t o = at; at += up(bytes, 256); return o; };
   f.hidden = take(s.copy_hidden ? s.T * s.Hp * s.es : 0);
@@ -77,25 +97,18 @@ struct Backward {
   bool h_direct;
   int64_t coef, largest, hidden, weight_copy, d, h_sums, w_sums, total;
 };
-// Splits of a sum over `k_tiles`, where `tiles` are too few for the device.
-int64_t splits_of(int64_t tiles, int64_t k_tiles) {
-  const int64_t want = (kUnits + tiles - 1) / tiles, most = k_tiles / 8;
-  return want < 2 || most < 2 ? 1 : want < most ? want : most;
-}
-int64_t tiles_of(TileShape t, int64_t M, int64_t N) {
-  return up(M, tile_m(t)) / tile_m(t) * (up(N, tile_n(t)) / tile_n(t));
-}
 Backward backward_plan(const Shape& s) {
   Backward b;
   const int64_t all = up(s.V, 256), most = kPieceBytes / (s.T * s.es) / 256 * 256;
   b.piece = most < 256 ? 256 : most < all ? most : all;
   b.pieces = (all + b.piece - 1) / b.piece;
-  b.derivs = wide_shape(b.piece, s.T);
-  b.rows = wide_shape(s.H, s.T);
-  b.weight = wide_shape(s.H, b.piece);
   const int64_t kK = 128 / s.es;
-  b.h_splits = splits_of(tiles_of(b.rows, s.H, s.T), b.piece / kK);
-  b.w_splits = splits_of(tiles_of(b.weight, s.H, b.piece), up(s.T, kK) / kK);
+  b.derivs = choose(s.type, b.piece, s.T, 1, 1).tile;
+  const Choice h = choose(s.type, s.H, s.T, b.piece / kK, 16), w = choose(s.type, s.H, b.piece, up(s.T, kK) / kK, 16);
+  b.rows = h.tile;
+  b.h_splits = h.splits;
+  b.weight = w.tile;
+  b.w_splits = w.splits;
   b.h_direct = b.pieces == 1 && b.h_splits == 1;
   int64_t at = 0;
   const auto take = [&](int64_t bytes) { const int64_t o = at; at += up(bytes, 256); return o; };
@@ -180,13 +193,8 @@ __global__ __launch_bounds__(1024) void k_linear_join(const float* __restrict__ 
   float s = 0.0f, x = 0.0f;
   if (on)
 #pragma unroll 4
-    for (int64_t i = share; i < slots; i += shares) {
-      const float d = (part[i * 3 * T + n] - ref) * c;
-      const float si = part[(i * 3 + 1) * T + n], xi = part[(i * 3 + 2) * T + n];
-      const float y = __builtin_amdgcn_exp2f(d);
-      s = fmaf(y, si, s);
-      x = fmaf(y, fmaf(si, fmaxf(d, -1e30f), xi), x);
-    }
+    for (int64_t i = share; i < slots; i += shares)
+      tile::join_sums(part[i * 3 * T + n], part[(i * 3 + 1) * T + n], part[(i * 3 + 2) * T + n], ref, c, s, x);
   red[tid] = s;
   red2[tid] = x;
   for (int w = 512; w >= tokens_here; w >>= 1) {
@@ -327,7 +335,7 @@ hipError_t launch_linear(const LinearArgs& a, hipStream_t st) {
   p.given = reinterpret_cast<float*>(w + f.given);
   if ((e = product(kFormLogprobs, p, s.type, f.tile, st)) != hipSuccess) return e;
   int log_n = 0;
-  while (log_n < 6 && ((int64_t)1 << log_n) < s.T) ++log_n;
+  while (log_n < 6 && ((int64_t)64 << log_n) < s.T) ++log_n;
   const unsigned grid = static_cast<unsigned>((s.T + ((int64_t)1 << log_n) - 1) >> log_n);
   k_linear_join<<<grid, 1024, 0, st>>>(p.part, f.slots, p.given, s.T, s.V, a.tokens, a.it, p.c, log_n,
                                        a.logprob, a.entropy, a.stats);

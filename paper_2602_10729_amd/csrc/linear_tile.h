@@ -48,7 +48,7 @@ struct TileArgs {
   // kLogprobs
   const int64_t* tokens;
   float c;                                // log2(e) inverse temperature
-  float* part;                            // [slots][3][N]
+  float* part;                            // [m-tiles][3][N]
   float* given;                           // [N]
   // kDerivs
   const TokenCoef* coef;                  // (kRows, kSums: of out's rows, or nullptr)
@@ -80,7 +80,7 @@ __device__ __forceinline__ float exp2i(int e) { return __uint_as_float(static_ca
 
 namespace tile {
 
-typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -102,6 +102,12 @@ __device__ __forceinline__ void load_lds(u32x4 buffer, uint32_t offset, uint32_t
 template <int N>
 __device__ __forceinline__ void wait_loads() {     // all but the last N; and LDS reads
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(N) : "memory");
+}
+
+// LDS accesses of a wave are done in order; this keeps the compiler to it.
+__device__ __forceinline__ void wave_order() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_wave_barrier();
 }
 
 // One operand's tile: R rows of its own index, kRowBytes of k, loaded by WAVES
@@ -152,9 +158,9 @@ struct Loader {
   __device__ __forceinline__ void load(uint32_t to) {
     const int64_t n = (left + 3) & ~int64_t(3);    // (the word that holds the last element)
     u32x4 buffer;
-    buffer[0] = static_cast<uint32_t>(base);
-    buffer[1] = static_cast<uint32_t>(base >> 32) & 0xFFFF;
-    buffer[2] = static_cast<uint32_t>(n < 0 ? 0 : n > kFar ? kFar : n);
+    buffer[0] = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(base));
+    buffer[1] = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(base >> 32) & 0xFFFF);
+    buffer[2] = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(n < 0 ? 0 : n > kFar ? kFar : n));
     buffer[3] = 0x00020000;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
@@ -164,20 +170,22 @@ struct Loader {
   }
 };
 
-// Fragments of one operand, 32 rows each, from a tile in LDS.
+// Fragments of one operand, 16 rows and 64 bytes of k each, from a tile in LDS:
+// lane l holds row l % 16 and the (l / 16)-th 16 bytes.
 template <int TYPE, bool ACROSS, int R>
 struct Reader {
   static constexpr int kBytes = sizeof(typename Elem<TYPE>::T);
+  static constexpr int kReads = !ACROSS ? 1 : kBytes == 2 ? 2 : 4;       // of a fragment
   int row0;                                        // of the wave
   __device__ __forceinline__ u32x4 get(const char* lds, int block, int j) const {
-    const int lane = threadIdx.x & 63;
+    const int lane = threadIdx.x & 63, i = lane & 15, part = lane >> 4;
     if constexpr (!ACROSS) {
-      const int r = row0 + block * 32 + (lane & 31);
-      const int g = (2 * j + (lane >> 5)) ^ (lane & 7);
+      const int r = row0 + block * 16 + i;
+      const int g = (4 * j + part) ^ (lane & 7);
       return *reinterpret_cast<const u32x4*>(lds + r * kRowBytes + g * 16);
     } else if constexpr (kBytes == 2) {
-      const int i = lane & 15, k = 16 * j + 8 * (lane >> 5) + (i >> 2);
-      const int unit = (row0 / 16 + block * 2 + ((lane >> 4) & 1)) ^ (i >> 2);
+      const int k = 32 * j + 8 * part + (i >> 2);
+      const int unit = (row0 / 16 + block) ^ (i >> 2);
       const char* at = lds + k * (R * 2) + unit * 32 + (i & 3) * 8;
       typedef __attribute__((address_space(3))) s16x4 LdsVec;
       const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsVec*)at);
@@ -190,8 +198,8 @@ struct Reader {
       u32x4 f;
 #pragma unroll
       for (int s = 0; s < 4; ++s) {
-        const int k = 8 * j + 4 * (lane >> 5) + s;
-        f[s] = *reinterpret_cast<const uint32_t*>(lds + k * (R * 4) + (row0 + block * 32 + (lane & 31)) * 4);
+        const int k = 16 * j + 4 * part + s;
+        f[s] = *reinterpret_cast<const uint32_t*>(lds + k * (R * 4) + (row0 + block * 16 + i) * 4);
       }
       return f;
     }
@@ -210,16 +218,19 @@ __device__ __forceinline__ u32x4 keep_first(u32x4 f, int n) {
   return f;
 }
 
+// 16 x 16 x 64 bytes. (The 32 x 32 products take as many operands from LDS for a
+// wave's tile, but more time: 28.3 against 26.9 ms for the training step of 8192 x
+// 128000 x 4096, where the clock follows the power drawn.)
 template <int TYPE>
-__device__ __forceinline__ f32x16 mma(u32x4 a, u32x4 b, f32x16 c) {
+__device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 c) {
   if constexpr (TYPE == BO_TYPE_BF16) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
   } else if constexpr (TYPE == BO_TYPE_F16) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
   } else {
 #pragma unroll
     for (int s = 0; s < 4; ++s)
-      c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[s]), __uint_as_float(b[s]), c, 0, 0, 0);
+      c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[s]), __uint_as_float(b[s]), c, 0, 0, 0);
     return c;
   }
 }
@@ -240,11 +251,18 @@ __device__ __forceinline__ void place(const TileArgs& p, int& mt, int& nt, int& 
   mt = group * kGroup + in % width;
 }
 
+// Adds sums relative to a maximum mi to s and x, which are relative to ref.
+__device__ __forceinline__ void join_sums(float mi, float si, float xi, float ref, float c, float& s, float& x) {
+  const float d = (mi - ref) * c, y = __builtin_amdgcn_exp2f(d);
+  s = fmaf(y, si, s);
+  x = fmaf(y, fmaf(si, fmaxf(d, -1e30f), xi), x);
+}
+
 // BM x BN tiles, WM x WN waves, a ring of STAGES k-tiles in LDS.
 template <int TYPE, bool AA, bool BA, Epilogue EPI, int BM, int BN, int WM, int WN, int STAGES>
 __global__ __launch_bounds__(64 * WM * WN) void k_tile(TileArgs p) {
   using E = typename Elem<TYPE>::T;
-  constexpr int kWaves = WM * WN, MI = BM / WM / 32, NI = BN / WN / 32;
+  constexpr int kWaves = WM * WN, MI = BM / WM / 16, NI = BN / WN / 16;
   constexpr int kStage = (BM + BN) * kRowBytes;
   constexpr int kK = kRowBytes / static_cast<int>(sizeof(E));
   using LoadA = Loader<TYPE, AA, BM, kWaves>;
@@ -262,206 +280,251 @@ __global__ __launch_bounds__(64 * WM * WN) void k_tile(TileArgs p) {
   LoadB lb;
   la.init(p.a, p.a_stride, static_cast<int64_t>(mt) * BM, p.M, p.K, kt0);
   lb.init(p.b, p.b_stride, static_cast<int64_t>(nt) * BN, p.N, p.K, kt0);
-  const Reader<TYPE, AA, BM> ra{wm * MI * 32};
-  const Reader<TYPE, BA, BN> rb{wn * NI * 32};
-  f32x16 acc[MI][NI];
+  const Reader<TYPE, AA, BM> ra{wm * MI * 16};
+  const Reader<TYPE, BA, BN> rb{wn * NI * 16};
+  f32x4 acc[MI][NI];
 #pragma unroll
   for (int i = 0; i < MI; ++i)
 #pragma unroll
-    for (int j = 0; j < NI; ++j)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+    for (int j = 0; j < NI; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   const uint32_t lds0 = lds_address(lds);
   const auto fetch = [&](int stage) {
     la.load(lds0 + stage * kStage);
     lb.load(lds0 + stage * kStage + BM * kRowBytes);
   };
-  const auto multiply = [&](const char* stage, auto masked, int n) {
+  // Fragments: all of B's and the latter half of A's twice, for a step and the
+  // next; the first half of A's is replaced once its products are issued.
+  constexpr int kHalf = MI / 2;
+  u32x4 first[kHalf], second[2][kHalf], fb[2][NI];
+  const auto read_most = [&](int stage, int j) {
+    const char* at = lds + stage * kStage;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      u32x4 a[MI], b[NI];
+    for (int i = 0; i < NI; ++i) fb[j][i] = rb.get(at + BM * kRowBytes, i, j);
 #pragma unroll
-      for (int i = 0; i < MI; ++i) a[i] = ra.get(stage, i, j);
-#pragma unroll
-      for (int i = 0; i < NI; ++i) b[i] = rb.get(stage + BM * kRowBytes, i, j);
-      if constexpr (decltype(masked)::value) {
-        const int keep = n - (2 * j + (lane >> 5)) * (kK / 8);
-#pragma unroll
-        for (int i = 0; i < MI; ++i) a[i] = keep_first<TYPE>(a[i], keep);
-#pragma unroll
-        for (int i = 0; i < NI; ++i) b[i] = keep_first<TYPE>(b[i], keep);
-      }
-#pragma unroll
-      for (int i = 0; i < MI; ++i)
-#pragma unroll
-        for (int l = 0; l < NI; ++l) acc[i][l] = mma<TYPE>(a[i], b[l], acc[i][l]);
-    }
+    for (int i = 0; i < kHalf; ++i) second[j][i] = ra.get(at, kHalf + i, j);
   };
-  // A k-tile is waited for, then (all waves being past the one before) the load
-  // of a later one takes that one's place, then it is multiplied. Past the end
-  // loads are issued all the same, out of range, so that counts stay the same.
+  const auto read_first = [&](int stage, int j) {
+#pragma unroll
+    for (int i = 0; i < kHalf; ++i) first[i] = ra.get(lds + stage * kStage, i, j);
+  };
+  const auto multiply = [&](const u32x4 (&a)[kHalf], int j, int i0) {
+#pragma unroll
+    for (int i = 0; i < kHalf; ++i)
+#pragma unroll
+      for (int l = 0; l < NI; ++l) acc[i0 + i][l] = mma<TYPE>(a[i], fb[j][l], acc[i0 + i][l]);
+  };
+  constexpr int kProducts = kHalf * NI * (TYPE == BO_TYPE_F32 ? 4 : 1);
+  const auto spread = [&](auto reads) {            // reads between products
+    constexpr int kAll = decltype(reads)::value, kEach = kProducts / kAll > 2 ? 2 : 1;
+#pragma unroll
+    for (int i = 0; i < kAll; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, kEach, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, kProducts, 0);
+  };
+  using Most = std::integral_constant<int, NI * decltype(rb)::kReads + kHalf * decltype(ra)::kReads>;
+  using First = std::integral_constant<int, kHalf * decltype(ra)::kReads>;
+  // A k-tile is two steps of 64 bytes; a step's fragments are read during the
+  // products of the one before. Between the two, every wave has all of the tile,
+  // the next one has arrived, and a load of the tile STAGES further on takes this
+  // one's place. Past the end loads are issued all the same, out of range, so
+  // that counts stay the same.
   if (kt0 < kt1) {
 #pragma unroll
-    for (int s = 0; s < STAGES - 1; ++s) fetch(s);
-    int at = 0, next = STAGES - 1;
-    // (products over tokens or d end in rows or columns of 0: nothing to clear)
-    constexpr bool kLast = EPI == kLogprobs || EPI == kDerivs;
-    for (int64_t kt = kt0; kt < kt1 - kLast; ++kt) {
+    for (int s = 0; s < STAGES; ++s) fetch(s);
+    wait_loads<(STAGES - 1) * kLoads>();
+    __builtin_amdgcn_s_barrier();
+    read_most(0, 0);
+    read_first(0, 0);
+    int at = 0;
+    for (int64_t kt = kt0; kt < kt1 - 1; ++kt) {
+      read_most(at, 1);
+      multiply(first, 0, 0);
+      spread(Most());
+      read_first(at, 1);
+      multiply(second[0], 0, kHalf);
+      spread(First());
       wait_loads<(STAGES - 2) * kLoads>();
       __builtin_amdgcn_s_barrier();
-      fetch(next);
-      multiply(lds + at * kStage, std::false_type(), 0);
+      fetch(at);
       at = at + 1 == STAGES ? 0 : at + 1;
-      next = next + 1 == STAGES ? 0 : next + 1;
+      read_most(at, 0);
+      multiply(first, 1, 0);
+      spread(Most());
+      read_first(at, 0);
+      multiply(second[1], 1, kHalf);
+      spread(First());
     }
-    if (kLast) {
-      wait_loads<(STAGES - 2) * kLoads>();
-      __builtin_amdgcn_s_barrier();
-      multiply(lds + at * kStage, std::true_type(), static_cast<int>(p.K - (kt1 - 1) * kK));
-    }
+    // (products over tokens or d end in rows or columns of 0: nothing to clear)
+    const int n = static_cast<int>(p.K - (kt1 - 1) * kK);
+    const auto clear = [&](int j) {
+      if constexpr (EPI == kLogprobs || EPI == kDerivs) {
+        const int keep = n - (4 * j + (lane >> 4)) * (kK / 8);
+#pragma unroll
+        for (int i = 0; i < kHalf; ++i) first[i] = keep_first<TYPE>(first[i], keep);
+#pragma unroll
+        for (int i = 0; i < kHalf; ++i) second[j][i] = keep_first<TYPE>(second[j][i], keep);
+#pragma unroll
+        for (int i = 0; i < NI; ++i) fb[j][i] = keep_first<TYPE>(fb[j][i], keep);
+      }
+    };
+    clear(0);
+    read_most(at, 1);
+    multiply(first, 0, 0);
+    read_first(at, 1);
+    multiply(second[0], 0, kHalf);
+    clear(1);
+    multiply(first, 1, 0);
+    multiply(second[1], 1, kHalf);
     wait_loads<0>();
   }
 
-  const int64_t mw = static_cast<int64_t>(mt) * BM + wm * MI * 32;     // the wave's first m and n
-  const int64_t nw = static_cast<int64_t>(nt) * BN + wn * NI * 32;
-  const int half = lane >> 5;
-  // element e of block i: m = mw + 32 i + 8 (e / 4) + 4 half + e % 4
+  const int64_t mw = static_cast<int64_t>(mt) * BM + wm * MI * 16;     // the wave's first m and n
+  const int64_t nw = static_cast<int64_t>(nt) * BN + wn * NI * 16;
+  const int part = lane >> 4;
+  __builtin_amdgcn_s_barrier();                    // LDS is free
+  // element e of block i, j: m = mw + 16 i + 4 part + e, n = nw + 16 j + lane % 16
   if constexpr (EPI == kLogprobs) {
-    const int64_t slot = static_cast<int64_t>(mt) * WM + wm;
-    const int rows = static_cast<int>(min<int64_t>(MI * 32, p.M - mw));
+    const int rows = static_cast<int>(min<int64_t>(MI * 16, p.M - mw));
+    float* join = reinterpret_cast<float*>(lds);   // [WM][3][BN]
 #pragma unroll
     for (int j = 0; j < NI; ++j) {
-      const int64_t n = nw + 32 * j + (lane & 31);
+      const int64_t n = nw + 16 * j + (lane & 15);
       const bool on = n < p.N;
-      if (rows < MI * 32) {
+      if (rows < MI * 16) {
 #pragma unroll
         for (int i = 0; i < MI; ++i)
 #pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (32 * i + 8 * (e / 4) + 4 * half + e % 4 >= rows) acc[i][j][e] = -__builtin_huge_valf();
+          for (int e = 0; e < 4; ++e)
+            if (16 * i + 4 * part + e >= rows) acc[i][j][e] = -__builtin_huge_valf();
       }
       float m = acc[0][j][0];
 #pragma unroll
       for (int i = 0; i < MI; ++i)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) m = fmaxf(m, acc[i][j][e]);
+        for (int e = 0; e < 4; ++e) m = fmaxf(m, acc[i][j][e]);
+      m = fmaxf(m, __shfl_xor(m, 16));
       m = fmaxf(m, __shfl_xor(m, 32));
       const float ref = m == -__builtin_huge_valf() ? 0.0f : m;
       float s = 0.0f, x = 0.0f;
 #pragma unroll
       for (int i = 0; i < MI; ++i)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
+        for (int e = 0; e < 4; ++e) {
           const float d = (acc[i][j][e] - ref) * p.c;
           const float y = __builtin_amdgcn_exp2f(d);
           s += y;
           x = fmaf(y, fmaxf(d, -1e30f), x);       // (0 times what is masked)
         }
+      s += __shfl_xor(s, 16);
+      x += __shfl_xor(x, 16);
       s += __shfl_xor(s, 32);
       x += __shfl_xor(x, 32);
-      if (on && half == 0) {
-        float* to = p.part + slot * 3 * p.N + n;
+      if (part == 0) {
+        float* to = join + wm * 3 * BN + wn * NI * 16 + 16 * j + lane;
         to[0] = m;
-        to[p.N] = s;
-        to[2 * p.N] = x;
+        to[BN] = s;
+        to[2 * BN] = x;
       }
       const int64_t tok = on && p.tokens ? p.tokens[n] - mw : -1;
-      const bool mine = tok >= 0 && tok < rows && ((tok >> 2) & 1) == half;
+      const bool mine = tok >= 0 && tok < rows && ((tok >> 2) & 3) == part;
       if (__ballot(mine)) {
         float v = 0.0f;
 #pragma unroll
         for (int i = 0; i < MI; ++i)
 #pragma unroll
-          for (int e = 0; e < 16; ++e)
-            v = 32 * i + 8 * (e / 4) + 4 * half + e % 4 == tok ? acc[i][j][e] : v;
+          for (int e = 0; e < 4; ++e) v = 16 * i + 4 * part + e == tok ? acc[i][j][e] : v;
         if (mine) p.given[n] = v;
       }
     }
-  }
-  if constexpr (EPI == kDerivs) {
-    const float scale = TYPE == BO_TYPE_F16 ? exp2i(deriv_exponent(p.largest)) : 1.0f;
-    const float c = p.c;
-    E* out = static_cast<E*>(p.out);
+    __syncthreads();
+    const int64_t n = static_cast<int64_t>(nt) * BN + threadIdx.x;
+    if (threadIdx.x < BN && n < p.N) {
+      const float* from = join + threadIdx.x;
+      float m = from[0];
+#pragma unroll
+      for (int w = 1; w < WM; ++w) m = fmaxf(m, from[w * 3 * BN]);
+      const float ref = m == -__builtin_huge_valf() ? 0.0f : m;
+      float s = 0.0f, x = 0.0f;
+#pragma unroll
+      for (int w = 0; w < WM; ++w) join_sums(from[w * 3 * BN], from[(w * 3 + 1) * BN], from[(w * 3 + 2) * BN], ref, p.c, s, x);
+      float* to = p.part + static_cast<int64_t>(mt) * 3 * p.N + n;
+      to[0] = m;
+      to[p.N] = s;
+      to[2 * p.N] = x;
+    }
+  } else {
+    // A block of 16 n goes through the wave's own part of LDS, so that it leaves in
+    // whole rows; granules are XORed with n against bank conflicts.
+    using S = std::conditional_t<EPI == kSums, float, E>;
+    constexpr int kGranules = MI * 16 * static_cast<int>(sizeof(S)) / 16, kSwizzle = kGranules < 16 ? kGranules - 1 : 15;
+    static_assert(kWaves * 16 * kGranules * 16 <= STAGES * kStage, "a block of every wave fits");
+    char* mine = lds + wave * (16 * kGranules * 16);
+    float scale = 1.0f;
+    if constexpr (TYPE == BO_TYPE_F16 && EPI == kDerivs) scale = exp2i(deriv_exponent(p.largest));
+    if constexpr (TYPE == BO_TYPE_F16 && EPI == kRows) scale = exp2i(-deriv_exponent(p.largest));
 #pragma unroll
     for (int j = 0; j < NI; ++j) {
-      const int64_t n = nw + 32 * j + (lane & 31);
+      const int64_t n = nw + 16 * j + (lane & 15);
       const bool on = n < p.N;
-      const TokenCoef q = p.coef[on ? n : 0];
-      const bool live = on && q.live;
-      const float ref = q.m == -__builtin_huge_valf() ? 0.0f : q.m;
-      const float is = p.it * scale;
-      const int64_t tok = q.token - (p.m0 + mw);
+      TokenCoef q;
+      if constexpr (EPI == kDerivs) q = p.coef[on ? n : 0];
+      bool live = on;
+      if constexpr (EPI == kDerivs) live = on && q.live;
+      if constexpr (EPI == kRows) live = on && (!p.coef || p.coef[n].live);
+      const float ref = EPI != kDerivs || q.m == -__builtin_huge_valf() ? 0.0f : q.m;
+      const int64_t tok = EPI == kDerivs ? q.token - (p.m0 + mw) : -1;
 #pragma unroll
-      for (int i = 0; i < MI; ++i)
+      for (int i = 0; i < MI; ++i) {
+        S h[4];
 #pragma unroll
-        for (int e4 = 0; e4 < 4; ++e4) {
-          float d[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int r = 32 * i + 8 * e4 + 4 * half + e;
-            const float u2 = (acc[i][j][4 * e4 + e] - ref) * c - q.ls * 1.44269504f;
+        for (int e = 0; e < 4; ++e) {
+          float v = acc[i][j][e];
+          if constexpr (EPI == kDerivs) {
+            const int r = 16 * i + 4 * part + e;
+            const float u2 = (v - ref) * p.c - q.ls * 1.44269504f;
             const float y = __builtin_amdgcn_exp2f(u2);
             const float lin = y == 0.0f ? 0.0f : fmaf(u2, 0.69314718f, q.entropy);
-            float v = -y * fmaf(q.gh, lin, q.g);
+            v = -y * fmaf(q.gh, lin, q.g);
             if (r == tok) v += q.g;
-            d[e] = live && mw + r < p.M ? v * is : 0.0f;
+            v = mw + r < p.M ? v * (p.it * scale) : 0.0f;
           }
-          if (on) {
-            E h[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) h[e] = Elem<TYPE>::store(d[e]);
-            __builtin_memcpy(out + n * p.out_stride + mw + 32 * i + 8 * e4 + 4 * half, h, sizeof(h));
-          }
+          if constexpr (EPI == kRows) v *= scale;
+          if constexpr (EPI == kSums) h[e] = v;
+          else h[e] = Elem<TYPE>::store(live ? v : 0.0f);
         }
-    }
-  }
-  if constexpr (EPI == kSums) {
-    float* out = static_cast<float*>(p.out) + split * p.out_split;
+        const int byte = (16 * i + 4 * part) * static_cast<int>(sizeof(S));
+        const int g = (byte >> 4) ^ (lane & kSwizzle);
+        __builtin_memcpy(mine + (lane & 15) * (kGranules * 16) + g * 16 + (byte & 15), h, sizeof(h));
+      }
+      wave_order();
 #pragma unroll
-    for (int j = 0; j < NI; ++j) {
-      const int64_t n = nw + 32 * j + (lane & 31);
-      if (n >= p.N) continue;
-#pragma unroll
-      for (int i = 0; i < MI; ++i)
-#pragma unroll
-        for (int e4 = 0; e4 < 4; ++e4) {
-          const int64_t m = mw + 32 * i + 8 * e4 + 4 * half;
-          if (m >= p.out_stride) continue;          // (rows are whole fours)
-          float4* to = reinterpret_cast<float4*>(out + n * p.out_stride + m);
-          float4 v = {acc[i][j][4 * e4], acc[i][j][4 * e4 + 1], acc[i][j][4 * e4 + 2], acc[i][j][4 * e4 + 3]};
+      for (int c = 0; c < kGranules / 4; ++c) {
+        const int at = c * 64 + lane, r = at / kGranules, g = at % kGranules;
+        const int64_t row = nw + 16 * j + r, m = mw + g * (16 / static_cast<int>(sizeof(S)));
+        u32x4 v = *reinterpret_cast<const u32x4*>(mine + r * (kGranules * 16) + (g ^ (r & kSwizzle)) * 16);
+        if (row >= p.N) continue;
+        S* to = static_cast<S*>(p.out) + (EPI == kSums ? split * p.out_split : 0) + row * p.out_stride + m;
+        if constexpr (EPI == kSums) {
+          if (m >= p.out_stride) continue;          // (rows are whole granules)
           if (p.add) {
-            const float4 o = *to;
-            v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
+            const u32x4 o = *reinterpret_cast<const u32x4*>(to);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) + __uint_as_float(o[e]));
           }
-          *to = v;
+          *reinterpret_cast<u32x4*>(to) = v;
+        } else if (EPI == kDerivs || m + 16 / static_cast<int>(sizeof(S)) <= p.M) {
+          __builtin_memcpy(to, &v, 16);
+        } else {
+          S h[16 / sizeof(S)];
+          __builtin_memcpy(h, &v, 16);
+#pragma unroll
+          for (int e = 0; e < 16 / static_cast<int>(sizeof(S)); ++e)
+            if (m + e < p.M) to[e] = h[e];
         }
-    }
-  }
-  if constexpr (EPI == kRows) {
-    const float scale = TYPE == BO_TYPE_F16 ? exp2i(-deriv_exponent(p.largest)) : 1.0f;
-    E* out = static_cast<E*>(p.out);
-#pragma unroll
-    for (int j = 0; j < NI; ++j) {
-      const int64_t n = nw + 32 * j + (lane & 31);
-      if (n >= p.N) continue;
-      const bool live = !p.coef || p.coef[n].live;
-#pragma unroll
-      for (int i = 0; i < MI; ++i)
-#pragma unroll
-        for (int e4 = 0; e4 < 4; ++e4) {
-          const int64_t m = mw + 32 * i + 8 * e4 + 4 * half;
-          E h[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) h[e] = Elem<TYPE>::store(live ? scale * acc[i][j][4 * e4 + e] : 0.0f);
-          E* to = out + n * p.out_stride + m;
-          if (m + 4 <= p.M) {
-            __builtin_memcpy(to, h, sizeof(h));
-          } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (m + e < p.M) to[e] = h[e];
-          }
-        }
+      }
+      wave_order();
     }
   }
 }
@@ -480,7 +543,6 @@ hipError_t launch(const TileArgs& p, hipStream_t st) {
 enum TileShape { kBig, kMiddle, kNarrow64, kNarrow32 };
 constexpr int tile_m(TileShape s) { return s == kBig ? 256 : 128; }
 constexpr int tile_n(TileShape s) { return s == kBig ? 256 : s == kMiddle ? 128 : s == kNarrow64 ? 64 : 32; }
-constexpr int tile_wave_rows(TileShape s) { return s == kBig ? 2 : s == kMiddle ? 2 : 4; }    // waves along m
 
 template <int TYPE, bool AA, bool BA, Epilogue EPI>
 hipError_t launch_tile(TileArgs p, TileShape shape, hipStream_t st) {
