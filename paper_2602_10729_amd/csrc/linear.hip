@@ -47,25 +47,25 @@ int64_t tiles_of(TileShape t, int64_t M, int64_t N) {
 }
 
 // The shape of the tiles and the splits of k that should take the least time: whole
-// rounds of workgroups (one large tile a compute unit, or two of the quarter's
-// size, which take 1.2 times as long for the same work), and for split sums their
-// way through memory. In microseconds: a large k-tile takes 1.7 (16 bits) or 7.2
-// (fp32), memory 4 bytes a picosecond.
+// rounds of workgroups, and for split sums their way through memory (4 bytes a
+// picosecond). A k-tile of as many tiles as a compute unit holds at once takes, in
+// microseconds, measured with each shape alone:
+constexpr double kTileTime[2][3] = {{1.65, 1.06, 0.96}, {7.2, 3.7, 2.86}};      // 16 bits, fp32; big, middle, small
 struct Choice {
   TileShape tile;
   int64_t splits;
-  double cost;
 };
 Choice choose(int type, int64_t M, int64_t N, int64_t k_tiles, int64_t most_splits) {
-  Choice best{kBig, 1, 1e300};
-  for (const TileShape t : {kBig, kMiddle}) {
-    const int64_t tiles = tiles_of(t, M, N), at_once = t == kBig ? kUnits : 2 * kUnits;
-    const double k_tile = (type == BO_TYPE_F32 ? 7.2 : 1.7) * (t == kBig ? 1.0 : 0.6);
+  Choice best{kBig, 1};
+  double least = 1e300;
+  for (const TileShape t : {kBig, kMiddle, kSmall}) {
+    const int64_t tiles = tiles_of(t, M, N), at_once = kUnits * tile_at_once(t);
+    const double k_tile = kTileTime[type == BO_TYPE_F32][t];
     for (int64_t s = 1; s <= most_splits && (s == 1 || s <= k_tiles / 8); ++s) {
       const double rounds = static_cast<double>((tiles * s + at_once - 1) / at_once);
-      const double sums = s == 1 ? 0.0 : 8e-6 * static_cast<double>(s) * static_cast<double>(M) * static_cast<double>(N) / 4.0;
-      const double cost = rounds * static_cast<double>((k_tiles + s - 1) / s) * k_tile + sums + (s > 1 ? 5.0 : 0.0);
-      if (cost < best.cost) best = {t, s, cost};
+      const double sums = s == 1 ? 0.0 : 5.0 + 2e-6 * static_cast<double>(s * M) * static_cast<double>(N);
+      const double cost = rounds * static_cast<double>((k_tiles + s - 1) / s) * k_tile + sums;
+      if (cost < least) least = cost, best = {t, s};
     }
   }
   return best;

@@ -93,10 +93,28 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) {
   return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const void*)p));
 }
 
-// 16 bytes a lane from buffer + offset to LDS at `to` + 16 lane.
-__device__ __forceinline__ void load_lds(u32x4 buffer, uint32_t offset, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-               :: "s"(to), "v"(offset), "s"(buffer) : "memory");
+// N times 16 bytes a lane from buffer + offset to LDS at `to` + 1024 i + 16 lane.
+// The compiler does not see that this reads the buffer's registers as memory
+// instructions do, so the five wait states after a vector instruction that wrote
+// one of them (as a readfirstlane does) stand here, and the one after m0's write.
+template <int N>
+__device__ __forceinline__ void load_lds(u32x4 buffer, const uint32_t (&offset)[N], uint32_t to) {
+  static_assert(N == 1 || N == 2 || N == 4, "loads of a wave");
+  if constexpr (N == 1) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                 :: "s"(to), "v"(offset[0]), "s"(buffer) : "memory");
+  } else if constexpr (N == 2) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %2, %4, 0 offen lds\n\t"
+                 "s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %3, %4, 0 offen lds"
+                 :: "s"(to), "s"(to + 1024), "v"(offset[0]), "v"(offset[1]), "s"(buffer) : "memory");
+  } else {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %4, %8, 0 offen lds\n\t"
+                 "s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %5, %8, 0 offen lds\n\t"
+                 "s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %6, %8, 0 offen lds\n\t"
+                 "s_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %7, %8, 0 offen lds"
+                 :: "s"(to), "s"(to + 1024), "s"(to + 2048), "s"(to + 3072), "v"(offset[0]), "v"(offset[1]),
+                    "v"(offset[2]), "v"(offset[3]), "s"(buffer) : "memory");
+  }
 }
 
 template <int N>
@@ -108,6 +126,15 @@ __device__ __forceinline__ void wait_loads() {     // all but the last N; and LD
 __device__ __forceinline__ void wave_order() {
   asm volatile("" ::: "memory");
   __builtin_amdgcn_wave_barrier();
+}
+
+// The transposing read takes 32 bytes of each of eight rows of k at once, four
+// together and four eight further on: XORed into the number of those 32 bytes,
+// these bits of k put them on all banks, of which a row of 64 columns spans half
+// (with k % 4 alone, 9.9e7 of the 2.0e8 cycles that LDS was at work were conflicts).
+template <int R>
+__device__ __forceinline__ int across_swizzle(int k) {
+  return R == 64 ? ((k >> 1) & 1) | ((k >> 2) & 2) : (k & 3) | ((k >> 1) & 4);
 }
 
 // One operand's tile: R rows of its own index, kRowBytes of k, loaded by WAVES
@@ -149,7 +176,7 @@ struct Loader {
         const int slot = (wave * kLoads + q) * 64 + lane;
         const int k = slot / kGranules;
         int g = slot % kGranules;
-        if constexpr (kBytes == 2) g ^= (k & 3) << 1;
+        if constexpr (kBytes == 2) g ^= across_swizzle<R>(k) << 1;
         offset[q] = within(k * stride + g * 16);
       }
     }
@@ -162,9 +189,7 @@ struct Loader {
     buffer[1] = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(base >> 32) & 0xFFFF);
     buffer[2] = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(n < 0 ? 0 : n > kFar ? kFar : n));
     buffer[3] = 0x00020000;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-#pragma unroll
-    for (int q = 0; q < kLoads; ++q) load_lds(buffer, offset[q], to + (wave * kLoads + q) * 1024);
+    load_lds(buffer, offset, to + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * (kLoads * 1024));
     base += step;
     left -= step;
   }
@@ -185,7 +210,7 @@ struct Reader {
       return *reinterpret_cast<const u32x4*>(lds + r * kRowBytes + g * 16);
     } else if constexpr (kBytes == 2) {
       const int k = 32 * j + 8 * part + (i >> 2);
-      const int unit = (row0 / 16 + block) ^ (i >> 2);
+      const int unit = (row0 / 16 + block) ^ across_swizzle<R>(k);
       const char* at = lds + k * (R * 2) + unit * 32 + (i & 3) * 8;
       typedef __attribute__((address_space(3))) s16x4 LdsVec;
       const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsVec*)at);
@@ -218,9 +243,9 @@ __device__ __forceinline__ u32x4 keep_first(u32x4 f, int n) {
   return f;
 }
 
-// 16 x 16 x 64 bytes. (The 32 x 32 products take as many operands from LDS for a
-// wave's tile, but more time: 28.3 against 26.9 ms for the training step of 8192 x
-// 128000 x 4096, where the clock follows the power drawn.)
+// 16 x 16 x 64 bytes. (32 x 32 products take as many operands from LDS for a wave's
+// tile, but more time, also without bank conflicts: 29.3 against 26.8 ms for the
+// training step of 8192 x 128000 x 4096.)
 template <int TYPE>
 __device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 c) {
   if constexpr (TYPE == BO_TYPE_BF16) {
@@ -415,8 +440,18 @@ __global__ __launch_bounds__(64 * WM * WN) void k_tile(TileArgs p) {
           const float d = (acc[i][j][e] - ref) * p.c;
           const float y = __builtin_amdgcn_exp2f(d);
           s += y;
-          x = fmaf(y, fmaxf(d, -1e30f), x);       // (0 times what is masked)
+          x = fmaf(y, d, x);
         }
+      if (__ballot(!(x == x))) {                  // 0 times what is masked is 0
+        x = 0.0f;
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float d = (acc[i][j][e] - ref) * p.c;
+            x = fmaf(__builtin_amdgcn_exp2f(d), fmaxf(d, -1e30f), x);
+          }
+      }
       s += __shfl_xor(s, 16);
       x += __shfl_xor(x, 16);
       s += __shfl_xor(s, 32);
@@ -468,31 +503,55 @@ __global__ __launch_bounds__(64 * WM * WN) void k_tile(TileArgs p) {
     for (int j = 0; j < NI; ++j) {
       const int64_t n = nw + 16 * j + (lane & 15);
       const bool on = n < p.N;
-      TokenCoef q;
-      if constexpr (EPI == kDerivs) q = p.coef[on ? n : 0];
       bool live = on;
-      if constexpr (EPI == kDerivs) live = on && q.live;
-      if constexpr (EPI == kRows) live = on && (!p.coef || p.coef[n].live);
-      const float ref = EPI != kDerivs || q.m == -__builtin_huge_valf() ? 0.0f : q.m;
-      const int64_t tok = EPI == kDerivs ? q.token - (p.m0 + mw) : -1;
+      if constexpr (EPI == kDerivs) {
+        const TokenCoef q = p.coef[on ? n : 0];
+        live = on && q.live;
+        const float ref = q.m == -__builtin_huge_valf() ? 0.0f : q.m;
+        const float ls = q.ls * 1.44269504f, hot = q.g * p.it * scale, g = -hot, gh = -(q.gh * p.it * scale);
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float u2 = fmaf(acc[i][j][e] - ref, p.c, -ls);
+            const float lin = fmaf(fmaxf(u2, -1e30f), 0.69314718f, q.entropy);      // (finite where p is 0)
+            acc[i][j][e] = __builtin_amdgcn_exp2f(u2) * fmaf(gh, lin, g);
+          }
+        const int64_t tok = q.token - (p.m0 + mw);
+        if (__ballot(q.token >= 0 && tok >= 0 && tok < MI * 16)) {
+#pragma unroll
+          for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[i][j][e] += 16 * i + 4 * part + e == tok ? hot : 0.0f;
+        }
+        if (mw + MI * 16 > p.M) {
+#pragma unroll
+          for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (mw + 16 * i + 4 * part + e >= p.M) acc[i][j][e] = 0.0f;
+        }
+      }
+      if constexpr (EPI == kRows) {
+        live = on && (!p.coef || p.coef[n].live);
+        if constexpr (TYPE == BO_TYPE_F16) {
+#pragma unroll
+          for (int i = 0; i < MI; ++i) acc[i][j] *= scale;
+        }
+      }
+      if (EPI != kSums && __ballot(on && !live)) {
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[i][j][e] = live ? acc[i][j][e] : 0.0f;
+      }
 #pragma unroll
       for (int i = 0; i < MI; ++i) {
         S h[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          float v = acc[i][j][e];
-          if constexpr (EPI == kDerivs) {
-            const int r = 16 * i + 4 * part + e;
-            const float u2 = (v - ref) * p.c - q.ls * 1.44269504f;
-            const float y = __builtin_amdgcn_exp2f(u2);
-            const float lin = y == 0.0f ? 0.0f : fmaf(u2, 0.69314718f, q.entropy);
-            v = -y * fmaf(q.gh, lin, q.g);
-            if (r == tok) v += q.g;
-            v = mw + r < p.M ? v * (p.it * scale) : 0.0f;
-          }
-          if constexpr (EPI == kRows) v *= scale;
-          if constexpr (EPI == kSums) h[e] = v;
-          else h[e] = Elem<TYPE>::store(live ? v : 0.0f);
+          if constexpr (EPI == kSums) h[e] = acc[i][j][e];
+          else h[e] = Elem<TYPE>::store(acc[i][j][e]);
         }
         const int byte = (16 * i + 4 * part) * static_cast<int>(sizeof(S));
         const int g = (byte >> 4) ^ (lane & kSwizzle);
@@ -540,9 +599,10 @@ hipError_t launch(const TileArgs& p, hipStream_t st) {
 }  // namespace tile
 
 // Shapes of tiles, m by n.
-enum TileShape { kBig, kMiddle, kNarrow64, kNarrow32 };
-constexpr int tile_m(TileShape s) { return s == kBig ? 256 : 128; }
-constexpr int tile_n(TileShape s) { return s == kBig ? 256 : s == kMiddle ? 128 : s == kNarrow64 ? 64 : 32; }
+enum TileShape { kBig, kMiddle, kSmall, kNarrow64, kNarrow32 };
+constexpr int tile_m(TileShape s) { return s == kBig ? 256 : s == kSmall ? 64 : 128; }
+constexpr int tile_n(TileShape s) { return s == kBig ? 256 : s == kNarrow64 ? 64 : s == kNarrow32 ? 32 : 128; }
+constexpr int tile_at_once(TileShape s) { return s == kBig ? 1 : s == kMiddle ? 2 : 3; }    // on a compute unit
 
 template <int TYPE, bool AA, bool BA, Epilogue EPI>
 hipError_t launch_tile(TileArgs p, TileShape shape, hipStream_t st) {
@@ -551,6 +611,7 @@ hipError_t launch_tile(TileArgs p, TileShape shape, hipStream_t st) {
   switch (shape) {
     case kBig: return tile::launch<TYPE, AA, BA, EPI, 256, 256, 2, 4, 2>(p, st);
     case kMiddle: return tile::launch<TYPE, AA, BA, EPI, 128, 128, 2, 2, 2>(p, st);
+    case kSmall: return tile::launch<TYPE, AA, BA, EPI, 64, 128, 2, 2, 2>(p, st);
     default: break;
   }
   if constexpr (EPI == kLogprobs) {
