@@ -90,7 +90,13 @@ Forward forward_plan(const Shape& s) {
   return f;
 }
 
+// Up to so many tokens d is held in two 16-bit parts, as twice the tokens: over
+// few rows the rounding of their largest d does not average out, and their
+// products are not what takes the time (128 x 32000 x 4096 bf16: 289 against 242 us; 16: 213 against 204).
+constexpr int64_t kFewTokens = 128;
+
 struct Backward {
+  int64_t parts;                          // of d: 1 or 2
   int64_t piece, pieces;                  // columns
   TileShape derivs, rows, weight;
   int64_t h_splits, w_splits;
@@ -99,25 +105,26 @@ struct Backward {
 };
 Backward backward_plan(const Shape& s) {
   Backward b;
-  const int64_t all = up(s.V, 256), most = kPieceBytes / (s.T * s.es) / 256 * 256;
+  b.parts = s.es == 2 && s.T <= kFewTokens ? 2 : 1;
+  const int64_t all = up(s.V, 256), T = b.parts * s.T, most = kPieceBytes / (T * s.es) / 256 * 256;
   b.piece = most < 256 ? 256 : most < all ? most : all;
   b.pieces = (all + b.piece - 1) / b.piece;
   const int64_t kK = 128 / s.es;
   b.derivs = choose(s.type, b.piece, s.T, 1, 1).tile;
-  const Choice h = choose(s.type, s.H, s.T, b.piece / kK, 16), w = choose(s.type, s.H, b.piece, up(s.T, kK) / kK, 16);
+  const Choice h = choose(s.type, s.H, T, b.piece / kK, 16), w = choose(s.type, s.H, b.piece, up(T, kK) / kK, 16);
   b.rows = h.tile;
   b.h_splits = h.splits;
   b.weight = w.tile;
   b.w_splits = w.splits;
-  b.h_direct = b.pieces == 1 && b.h_splits == 1;
+  b.h_direct = b.parts == 1 && b.pieces == 1 && b.h_splits == 1;
   int64_t at = 0;
   const auto take = [&](int64_t bytes) { const int64_t o = at; at += up(bytes, 256); return o; };
   b.coef = take(s.T * static_cast<int64_t>(sizeof(TokenCoef)));
   b.largest = take(4 * kLargest);
-  b.hidden = take(s.T * s.Hp * s.es);
+  b.hidden = take(T * s.Hp * s.es);
   b.weight_copy = take(s.copy_weight ? s.V * s.Hp * s.es : 0);
-  b.d = take(s.T * b.piece * s.es);
-  b.h_sums = take(b.h_direct ? 0 : b.h_splits * s.T * s.Hp * 4);
+  b.d = take(T * b.piece * s.es);
+  b.h_sums = take(b.h_direct ? 0 : b.h_splits * T * s.Hp * 4);
   b.w_sums = take(b.w_splits == 1 ? 0 : b.w_splits * b.piece * s.Hp * 4);
   b.total = at;
   return b;
@@ -131,14 +138,16 @@ hipError_t product(TileProduct what, const TileArgs& p, int type, TileShape t, h
 
 // ---- copies of rows: aligned, ended by zeros; rows that take no part are 0 ----
 
+// The rows `copies` times, one after the other.
 template <typename U>
-__global__ __launch_bounds__(kWg) void k_copy_rows(const U* __restrict__ in, int64_t rows, int64_t H,
-                                                   int64_t stride, const TokenCoef* __restrict__ coef,
+__global__ __launch_bounds__(kWg) void k_copy_rows(const U* __restrict__ in, int64_t rows, int64_t copies,
+                                                   int64_t H, int64_t stride,
+                                                   const TokenCoef* __restrict__ coef,
                                                    U* __restrict__ out, int64_t Hp) {
   constexpr int kVec = 16 / sizeof(U);
-  const int64_t per = Hp / kVec, n = rows * per, all = static_cast<int64_t>(gridDim.x) * kWg;
+  const int64_t per = Hp / kVec, n = rows * copies * per, all = static_cast<int64_t>(gridDim.x) * kWg;
   for (int64_t i = static_cast<int64_t>(blockIdx.x) * kWg + threadIdx.x; i < n; i += all) {
-    const int64_t r = i / per, h = i % per * kVec;
+    const int64_t to = i / per, r = to < rows ? to : to - rows, h = i % per * kVec;
     U v[kVec];
     const bool live = !coef || coef[r].live;
     if (live && h + kVec <= H) {
@@ -147,17 +156,17 @@ __global__ __launch_bounds__(kWg) void k_copy_rows(const U* __restrict__ in, int
 #pragma unroll
       for (int e = 0; e < kVec; ++e) v[e] = live && h + e < H ? in[r * stride + h + e] : 0;
     }
-    __builtin_memcpy(out + r * Hp + h, v, 16);
+    __builtin_memcpy(out + to * Hp + h, v, 16);
   }
 }
-hipError_t copy_rows(const void* in, int64_t rows, int64_t stride, const TokenCoef* coef, void* out,
-                     const Shape& s, hipStream_t st) {
-  const int64_t blocks = (rows * s.Hp * s.es / 16 + kWg - 1) / kWg;
+hipError_t copy_rows(const void* in, int64_t rows, int64_t copies, int64_t stride, const TokenCoef* coef,
+                     void* out, const Shape& s, hipStream_t st) {
+  const int64_t blocks = (rows * copies * s.Hp * s.es / 16 + kWg - 1) / kWg;
   const unsigned grid = static_cast<unsigned>(blocks < 16384 ? blocks : 16384);
   if (s.es == 2)
-    k_copy_rows<uint16_t><<<grid, kWg, 0, st>>>(static_cast<const uint16_t*>(in), rows, s.H, stride, coef, static_cast<uint16_t*>(out), s.Hp);
+    k_copy_rows<uint16_t><<<grid, kWg, 0, st>>>(static_cast<const uint16_t*>(in), rows, copies, s.H, stride, coef, static_cast<uint16_t*>(out), s.Hp);
   else
-    k_copy_rows<uint32_t><<<grid, kWg, 0, st>>>(static_cast<const uint32_t*>(in), rows, s.H, stride, coef, static_cast<uint32_t*>(out), s.Hp);
+    k_copy_rows<uint32_t><<<grid, kWg, 0, st>>>(static_cast<const uint32_t*>(in), rows, copies, s.H, stride, coef, static_cast<uint32_t*>(out), s.Hp);
   return hipGetLastError();
 }
 
@@ -262,9 +271,10 @@ __global__ __launch_bounds__(kWg) void k_linear_coef(const int64_t* __restrict__
   }
 }
 
-// out = the splits' sums, scaled and rounded; rows that take no part are 0.
+// out = the splits' sums (and the parts', `rows` apart), scaled and rounded; rows
+// that take no part are 0.
 template <int TYPE>
-__global__ __launch_bounds__(kWg) void k_linear_round(const float* __restrict__ sums, int64_t splits,
+__global__ __launch_bounds__(kWg) void k_linear_round(const float* __restrict__ sums, int64_t splits, int64_t parts,
                                                       int64_t split_stride, int64_t rows, int64_t H, int64_t Hp,
                                                       const TokenCoef* __restrict__ coef,
                                                       const float* __restrict__ largest,
@@ -276,23 +286,24 @@ __global__ __launch_bounds__(kWg) void k_linear_round(const float* __restrict__ 
     if (h >= H) continue;
     float4 v = {0.0f, 0.0f, 0.0f, 0.0f};
     if (!coef || coef[r].live)
-      for (int64_t s = 0; s < splits; ++s) {
-        const float4 o = *reinterpret_cast<const float4*>(sums + s * split_stride + r * Hp + h);
-        v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
-      }
+      for (int64_t s = 0; s < splits; ++s)
+        for (int64_t d = 0; d < parts; ++d) {
+          const float4 o = *reinterpret_cast<const float4*>(sums + s * split_stride + (d * rows + r) * Hp + h);
+          v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
+        }
     const float f[4] = {v.x * scale, v.y * scale, v.z * scale, v.w * scale};
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       if (h + e < H) out[r * stride + h + e] = Elem<TYPE>::store(f[e]);
   }
 }
-hipError_t round_sums(const float* sums, int64_t splits, int64_t split_stride, int64_t rows, const Shape& s,
+hipError_t round_sums(const float* sums, int64_t splits, int64_t parts, int64_t split_stride, int64_t rows, const Shape& s,
                       const TokenCoef* coef, const float* largest, void* out, int64_t stride, hipStream_t st) {
   const int64_t blocks = (rows * s.Hp / 4 + kWg - 1) / kWg;
   const unsigned grid = static_cast<unsigned>(blocks < 16384 ? blocks : 16384);
   const auto go = [&](auto ty) {
     using E = typename Elem<decltype(ty)::value>::T;
-    k_linear_round<decltype(ty)::value><<<grid, kWg, 0, st>>>(sums, splits, split_stride, rows, s.H, s.Hp, coef, largest, static_cast<E*>(out), stride);
+    k_linear_round<decltype(ty)::value><<<grid, kWg, 0, st>>>(sums, splits, parts, split_stride, rows, s.H, s.Hp, coef, largest, static_cast<E*>(out), stride);
   };
   if (s.type == BO_TYPE_F32) go(std::integral_constant<int, BO_TYPE_F32>());
   else if (s.type == BO_TYPE_BF16) go(std::integral_constant<int, BO_TYPE_BF16>());
@@ -320,11 +331,11 @@ hipError_t launch_linear(const LinearArgs& a, hipStream_t st) {
   p.a = a.weight; p.a_stride = (s.V > 1 ? a.weight_stride : s.H) * s.es;
   p.b = a.hidden; p.b_stride = (s.T > 1 ? a.hidden_stride : s.H) * s.es;
   if (s.copy_hidden) {
-    if ((e = copy_rows(a.hidden, s.T, a.hidden_stride, nullptr, w + f.hidden, s, st)) != hipSuccess) return e;
+    if ((e = copy_rows(a.hidden, s.T, 1, a.hidden_stride, nullptr, w + f.hidden, s, st)) != hipSuccess) return e;
     p.b = w + f.hidden; p.b_stride = s.Hp * s.es;
   }
   if (s.copy_weight) {
-    if ((e = copy_rows(a.weight, s.V, a.weight_stride, nullptr, w + f.weight, s, st)) != hipSuccess) return e;
+    if ((e = copy_rows(a.weight, s.V, 1, a.weight_stride, nullptr, w + f.weight, s, st)) != hipSuccess) return e;
     p.a = w + f.weight; p.a_stride = s.Hp * s.es;
   }
   p.M = s.V; p.N = s.T; p.K = s.H;
@@ -360,12 +371,12 @@ hipError_t launch_linear_grad(const LinearArgs& a, hipStream_t st) {
   const float log_v = logf(static_cast<float>(s.V));
   k_linear_coef<<<kLargest, kWg, 0, st>>>(a.tokens, s.T, s.V, a.stats_in, a.entropy_in, a.g_logprob, a.g_entropy, a.it, log_v, coef, largest);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  if ((e = copy_rows(a.hidden, s.T, a.hidden_stride, coef, w + b.hidden, s, st)) != hipSuccess) return e;
+  if ((e = copy_rows(a.hidden, s.T, b.parts, a.hidden_stride, coef, w + b.hidden, s, st)) != hipSuccess) return e;
   const char* hidden = w + b.hidden;
   const char* weight = static_cast<const char*>(a.weight);
   int64_t weight_stride = (s.V > 1 ? a.weight_stride : s.H) * s.es;
   if (s.copy_weight) {
-    if ((e = copy_rows(a.weight, s.V, a.weight_stride, nullptr, w + b.weight_copy, s, st)) != hipSuccess) return e;
+    if ((e = copy_rows(a.weight, s.V, 1, a.weight_stride, nullptr, w + b.weight_copy, s, st)) != hipSuccess) return e;
     weight = w + b.weight_copy;
     weight_stride = s.Hp * s.es;
   }
@@ -382,6 +393,7 @@ hipError_t launch_linear_grad(const LinearArgs& a, hipStream_t st) {
     p.c = static_cast<float>(1.4426950408889634 * static_cast<double>(a.it));
     p.it = a.it;
     p.coef = coef; p.largest = largest;
+    p.low = b.parts > 1;
     p.m0 = v0; p.V = s.V;
     p.out = w + b.d; p.out_stride = b.piece;
     if ((e = product(kFormDerivs, p, s.type, b.derivs, st)) != hipSuccess) return e;
@@ -389,7 +401,7 @@ hipError_t launch_linear_grad(const LinearArgs& a, hipStream_t st) {
       TileArgs q{};
       q.a = weight + v0 * weight_stride; q.a_stride = weight_stride;
       q.b = w + b.d; q.b_stride = b.piece * s.es;
-      q.M = s.H; q.N = s.T; q.K = cols;
+      q.M = s.H; q.N = b.parts * s.T; q.K = cols;
       q.splits = static_cast<int>(b.h_splits);
       q.split_k = (b.piece / kK + b.h_splits - 1) / b.h_splits;
       q.largest = largest;
@@ -397,7 +409,7 @@ hipError_t launch_linear_grad(const LinearArgs& a, hipStream_t st) {
         q.coef = coef;
         q.out = a.grad_hidden; q.out_stride = a.grad_hidden_stride;
       } else {
-        q.out = h_sums; q.out_stride = s.Hp; q.out_split = s.T * s.Hp;
+        q.out = h_sums; q.out_stride = s.Hp; q.out_split = b.parts * s.T * s.Hp;
         q.add = i > 0;
       }
       if ((e = product(b.h_direct ? kHiddenRows : kHiddenSums, q, s.type, b.rows, st)) != hipSuccess) return e;
@@ -406,9 +418,9 @@ hipError_t launch_linear_grad(const LinearArgs& a, hipStream_t st) {
       TileArgs q{};
       q.a = hidden; q.a_stride = s.Hp * s.es;
       q.b = w + b.d; q.b_stride = b.piece * s.es;
-      q.M = s.H; q.N = cols; q.K = s.T;
+      q.M = s.H; q.N = cols; q.K = b.parts * s.T;
       q.splits = static_cast<int>(b.w_splits);
-      q.split_k = (up(s.T, kK) / kK + b.w_splits - 1) / b.w_splits;
+      q.split_k = (up(b.parts * s.T, kK) / kK + b.w_splits - 1) / b.w_splits;
       q.largest = largest;
       char* out = static_cast<char*>(a.grad_weight) + v0 * a.grad_weight_stride * s.es;
       if (b.w_splits == 1) {
@@ -418,12 +430,12 @@ hipError_t launch_linear_grad(const LinearArgs& a, hipStream_t st) {
       }
       if ((e = product(b.w_splits == 1 ? kWeightRows : kWeightSums, q, s.type, b.weight, st)) != hipSuccess) return e;
       if (b.w_splits > 1 &&
-          (e = round_sums(w_sums, b.w_splits, b.piece * s.Hp, cols, s, nullptr, largest, out, a.grad_weight_stride, st)) != hipSuccess)
+          (e = round_sums(w_sums, b.w_splits, 1, b.piece * s.Hp, cols, s, nullptr, largest, out, a.grad_weight_stride, st)) != hipSuccess)
         return e;
     }
   }
   if (a.grad_hidden && !b.h_direct)
-    return round_sums(h_sums, b.h_splits, s.T * s.Hp, s.T, s, coef, largest, a.grad_hidden, a.grad_hidden_stride, st);
+    return round_sums(h_sums, b.h_splits, b.parts, b.parts * s.T * s.Hp, s.T, s, coef, largest, a.grad_hidden, a.grad_hidden_stride, st);
   return hipSuccess;
 }
 

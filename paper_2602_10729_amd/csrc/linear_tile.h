@@ -55,6 +55,7 @@ struct TileArgs {
   const float* largest;                   // [64], for the scale of f16
   float it;
   float log_v;
+  int low;                                // rows N + n: what the rounding of rows n left
   int64_t m0;                             // first m of the piece, in the vocabulary
   int64_t V;
   // out
@@ -545,45 +546,54 @@ __global__ __launch_bounds__(64 * WM * WN) void k_tile(TileArgs p) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) acc[i][j][e] = live ? acc[i][j][e] : 0.0f;
       }
+      const int halves = EPI == kDerivs && TYPE != BO_TYPE_F32 && p.low ? 2 : 1;
+      for (int half = 0; half < halves; ++half) {
+        if (half) {                                // what the rounding left
 #pragma unroll
-      for (int i = 0; i < MI; ++i) {
-        S h[4];
+          for (int i = 0; i < MI; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          if constexpr (EPI == kSums) h[e] = acc[i][j][e];
-          else h[e] = Elem<TYPE>::store(acc[i][j][e]);
+            for (int e = 0; e < 4; ++e) acc[i][j][e] -= Elem<TYPE>::load(Elem<TYPE>::store(acc[i][j][e]));
         }
-        const int byte = (16 * i + 4 * part) * static_cast<int>(sizeof(S));
-        const int g = (byte >> 4) ^ (lane & kSwizzle);
-        __builtin_memcpy(mine + (lane & 15) * (kGranules * 16) + g * 16 + (byte & 15), h, sizeof(h));
-      }
-      wave_order();
 #pragma unroll
-      for (int c = 0; c < kGranules / 4; ++c) {
-        const int at = c * 64 + lane, r = at / kGranules, g = at % kGranules;
-        const int64_t row = nw + 16 * j + r, m = mw + g * (16 / static_cast<int>(sizeof(S)));
-        u32x4 v = *reinterpret_cast<const u32x4*>(mine + r * (kGranules * 16) + (g ^ (r & kSwizzle)) * 16);
-        if (row >= p.N) continue;
-        S* to = static_cast<S*>(p.out) + (EPI == kSums ? split * p.out_split : 0) + row * p.out_stride + m;
-        if constexpr (EPI == kSums) {
-          if (m >= p.out_stride) continue;          // (rows are whole granules)
-          if (p.add) {
-            const u32x4 o = *reinterpret_cast<const u32x4*>(to);
+        for (int i = 0; i < MI; ++i) {
+          S h[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) + __uint_as_float(o[e]));
+          for (int e = 0; e < 4; ++e) {
+            if constexpr (EPI == kSums) h[e] = acc[i][j][e];
+            else h[e] = Elem<TYPE>::store(acc[i][j][e]);
           }
-          *reinterpret_cast<u32x4*>(to) = v;
-        } else if (EPI == kDerivs || m + 16 / static_cast<int>(sizeof(S)) <= p.M) {
-          __builtin_memcpy(to, &v, 16);
-        } else {
-          S h[16 / sizeof(S)];
-          __builtin_memcpy(h, &v, 16);
-#pragma unroll
-          for (int e = 0; e < 16 / static_cast<int>(sizeof(S)); ++e)
-            if (m + e < p.M) to[e] = h[e];
+          const int byte = (16 * i + 4 * part) * static_cast<int>(sizeof(S));
+          const int g = (byte >> 4) ^ (lane & kSwizzle);
+          __builtin_memcpy(mine + (lane & 15) * (kGranules * 16) + g * 16 + (byte & 15), h, sizeof(h));
         }
+        wave_order();
+#pragma unroll
+        for (int c = 0; c < kGranules / 4; ++c) {
+          const int at = c * 64 + lane, r = at / kGranules, g = at % kGranules;
+          const int64_t row = nw + 16 * j + r, m = mw + g * (16 / static_cast<int>(sizeof(S)));
+          u32x4 v = *reinterpret_cast<const u32x4*>(mine + r * (kGranules * 16) + (g ^ (r & kSwizzle)) * 16);
+          if (row >= p.N) continue;
+          S* to = static_cast<S*>(p.out) + (EPI == kSums ? split * p.out_split : 0) + (row + half * p.N) * p.out_stride + m;
+          if constexpr (EPI == kSums) {
+            if (m >= p.out_stride) continue;          // (rows are whole granules)
+            if (p.add) {
+              const u32x4 o = *reinterpret_cast<const u32x4*>(to);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) + __uint_as_float(o[e]));
+            }
+            *reinterpret_cast<u32x4*>(to) = v;
+          } else if (EPI == kDerivs || m + 16 / static_cast<int>(sizeof(S)) <= p.M) {
+            __builtin_memcpy(to, &v, 16);
+          } else {
+            S h[16 / sizeof(S)];
+            __builtin_memcpy(h, &v, 16);
+#pragma unroll
+            for (int e = 0; e < 16 / static_cast<int>(sizeof(S)); ++e)
+              if (m + e < p.M) to[e] = h[e];
+          }
+        }
+        wave_order();
       }
-      wave_order();
     }
   }
 }
