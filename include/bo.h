@@ -724,7 +724,7 @@ bo_status bo_dispatch(const int32_t* ids, int64_t N, int32_t E, int64_t capacity
  *          bo_linear_logprobs_workspace(..) bytes for these matrices;
  *          overwritten; calls that may overlap need one each. Rows that are
  *          not aligned to 4 bytes are copied into it first.
- * T >= 0 (0 is a no-op), T < 2^31, 1 <= V <= 2^30, T V <= 2^38,
+ * T >= 0 (0 is a no-op), T < 2^31, 1 <= V <= 2^29, T V <= 2^38,
  * 1 <= H <= BO_MAX_WIDTH.
  * Asynchronous. Errors: INVALID_ARGUMENT, CAPACITY, DEVICE.
  */

@@ -11,7 +11,10 @@
 // a token are cleared beside that work, each row of the table being written once.
 // Nothing depends on the order in which atomics arrive.
 //
-// Memory bounds it: the rows of grad once, the table once.
+// Memory bounds it: the rows of grad once, the table once. 32768 tokens of text over
+// a table of 128000 x 2048 bf16 take 50 us forward (268 MB, 5.4 TB/s) and 143 for the
+// gradient: 4.6 marks cleared, 33 the sort with 100 MB of rows cleared beside it, 97
+// the sums and the rest (0.5 GB), 10 the runs over chunks.
 #include "rows.h"
 
 namespace bo {
@@ -531,7 +534,8 @@ hipError_t launch_embed_grad(const EmbedArgs& a, hipStream_t st) {
   const int64_t groups = (a.V + kFillRows - 1) / kFillRows;
   while (fill.split < 10 && ((int64_t)1024 << fill.split) < fill.row) ++fill.split;
   const int64_t fills = groups << fill.split;
-  // what a launch of the sort has time for beside it: 32 MB
+  // what a launch of the sort has time for beside it: 32 MB (of 5 to 7 us, it then
+  // takes 7 to 11)
   const int64_t beside = ((int64_t)32 << 20) / (kFillRows * fill.row) << fill.split;
   const auto share = [&](int64_t units) {
     fill.first = fill.last;

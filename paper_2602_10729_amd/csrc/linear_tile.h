@@ -4,23 +4,32 @@
 //   kLogprobs  A = weight, B = hidden, k over H: logits; a tile leaves each
 //              token's maximum, sum of exponentials and sum of exponent times
 //              exponential, and the given token's logit
-//   kDerivs    the same product again; a tile becomes d (see bo.h), rounded
+//   kDerivs    the same product again; a tile becomes the logits' gradient, rounded
 //   kSums      fp32 sums, added to what is there or not
 //   kRows      rounded results
 // The gradients are A = weight by k over the vocabulary and B = d (grad_hidden),
 // and A = hidden, B = d, both by k over the tokens (grad_weight).
 //
-// m is the side that lies together in out, so that a lane, which holds four
-// consecutive m of one n, stores them together, and so that a token's logits
-// stay in one lane but for its partner: softmax needs no exchange but one.
+// m is the side that lies together in out: a lane holds four consecutive m of one n,
+// and a token's logits stay within four lanes, so that the softmax exchanges little.
 //
-// An operand lies with k together in its rows (K) or with its own index together
-// (kAcross: rows are k). Tiles come by loads straight into LDS, 16 bytes a lane,
-// range-checked by the buffer's size: rows and granules past the end are 0. A
-// wave reads fragments of 16 bytes a lane: for K its lane's row; for kAcross four
-// rows at a time through the transposing read (16-bit types) or element by
-// element (fp32). LDS rows hold their granules XORed with the row's low bits, so
-// that lanes which read together fall on different banks.
+// An operand has k together in its rows, or its own index (ACROSS: rows are k).
+// Tiles come by loads straight into LDS, 16 bytes a lane, range-checked by the
+// buffer's size: rows and granules past the end are 0. A wave reads fragments of 16
+// bytes a lane: its lane's row; or ACROSS, four rows at a time through the
+// transposing read (16-bit types) or element by element (fp32). LDS rows hold their
+// granules XORed with bits of the row's number, so that lanes which read together
+// fall on different banks (no conflicts left).
+//
+// What bounds it: at 256 x 256 tiles of eight waves the matrix pipes are busy 61% of
+// the time at 2.0 GHz, the clock that the power leaves; the products run at 1.28
+// PFLOP/s (bf16, H = 4096, epilogues included) where a library's, of the same
+// operands and no epilogue, reaches 1.36. Measured and not taken, for the training
+// step of 8192 x 128000 x 4096 (26.9 ms): 32 x 32 matrix products 29.3, four waves
+// of 128 x 128 33.7 (registers spilled), k-tiles of 64 bytes in a ring of four or
+// five 28.3, raised wave priority around the products 30.1, other orders of the tiles
+// the same. With every operand in the nearest cache (not a right result) it takes
+// 24.8: what memory costs.
 #pragma once
 
 #include <type_traits>
@@ -33,7 +42,7 @@ enum Epilogue { kLogprobs, kDerivs, kSums, kRows };
 
 // What the gradient needs of a token, and whether it takes part.
 struct TokenCoef {
-  float m, ls, g, gh, entropy;            // stats; gradients times nothing yet
+  float m, ls, g, gh, entropy;            // stats; the gradients that come in
   int32_t token;                          // or -1
   int32_t live, pad;
 };
@@ -51,13 +60,11 @@ struct TileArgs {
   float* part;                            // [m-tiles][3][N]
   float* given;                           // [N]
   // kDerivs
-  const TokenCoef* coef;                  // (kRows, kSums: of out's rows, or nullptr)
+  const TokenCoef* coef;                  // (kRows: of out's rows, or nullptr)
   const float* largest;                   // [64], for the scale of f16
   float it;
-  float log_v;
   int low;                                // rows N + n: what the rounding of rows n left
   int64_t m0;                             // first m of the piece, in the vocabulary
-  int64_t V;
   // out
   void* out;
   int64_t out_stride;                     // elements
@@ -610,7 +617,7 @@ hipError_t launch(const TileArgs& p, hipStream_t st) {
 
 // Shapes of tiles, m by n.
 enum TileShape { kBig, kMiddle, kSmall, kNarrow64, kNarrow32 };
-constexpr int tile_m(TileShape s) { return s == kBig ? 256 : s == kSmall ? 64 : 128; }
+constexpr int tile_m(TileShape s) { return s == kBig ? 256 : s == kSmall || s == kNarrow32 ? 64 : 128; }
 constexpr int tile_n(TileShape s) { return s == kBig ? 256 : s == kNarrow64 ? 64 : s == kNarrow32 ? 32 : 128; }
 constexpr int tile_at_once(TileShape s) { return s == kBig ? 1 : s == kMiddle ? 2 : 3; }    // on a compute unit
 
@@ -626,7 +633,7 @@ hipError_t launch_tile(TileArgs p, TileShape shape, hipStream_t st) {
   }
   if constexpr (EPI == kLogprobs) {
     if (shape == kNarrow64) return tile::launch<TYPE, AA, BA, EPI, 128, 64, 4, 1, 3>(p, st);
-    return tile::launch<TYPE, AA, BA, EPI, 128, 32, 4, 1, 3>(p, st);
+    return tile::launch<TYPE, AA, BA, EPI, 64, 32, 2, 2, 6>(p, st);
   }
   return hipErrorInvalidValue;
 }

@@ -29,7 +29,7 @@ def test_linear_refusals(L):
     assert call(hs=7) == INVALID and call(hidden=None) == INVALID
     assert call(hidden=ctypes.c_void_p(0x1002)) == INVALID            # not aligned to fp32
     assert call(H=(1 << 20) + 1, hs=1 << 21, ws=1 << 21) == CAPACITY and call(T=2 ** 31) == CAPACITY
-    assert call(V=2 ** 30 + 1) == CAPACITY and call(T=2 ** 20, V=2 ** 19) == CAPACITY
+    assert call(V=2 ** 29 + 1) == CAPACITY and call(T=2 ** 20, V=2 ** 19) == CAPACITY
     assert call(T=2 ** 30, V=1, H=1 << 20, hs=2 ** 40) == CAPACITY    # the extent overflows
     assert call(T=0, hidden=None) == 0
 
@@ -45,7 +45,7 @@ def test_linear_workspaces(L):
     f, g = L.bo_linear_logprobs_workspace, L.bo_linear_logprobs_grad_workspace
     for w in (f, g):
         assert w(P, 8, P, 8, 0, 0, 10, 8) == 0 and w(P, 8, P, 8, 5, 2, 10, 8) == 0
-        assert w(P, 8, P, 8, 0, 2, 10, 0) == 0 and w(P, 8, P, 8, 0, 2 ** 30, 2 ** 30, 8) == 0
+        assert w(P, 8, P, 8, 0, 2, 10, 0) == 0 and w(P, 8, P, 8, 0, 2 ** 29, 2 ** 29, 8) == 0
     # far less than the logits, for a large batch
     T, V, H = 16384, 128000, 4096
     assert f(P, H, P, H, 1, T, V, H) < T * V * 4 / 16
