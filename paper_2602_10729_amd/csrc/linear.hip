@@ -362,6 +362,7 @@ hipError_t launch_linear(const LinearArgs& a, hipStream_t st) {
 }
 
 hipError_t launch_linear_grad(const LinearArgs& a, hipStream_t st) {
+  if (!a.grad_hidden && !a.grad_weight) return hipSuccess;
   const Shape s = shape_of(a);
   if (s.T == 0) {
     if (!a.grad_weight) return hipSuccess;

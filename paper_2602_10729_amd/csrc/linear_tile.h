@@ -27,8 +27,9 @@
 // operands and no epilogue, reaches 1.36. Measured and not taken, for the training
 // step of 8192 x 128000 x 4096 (26.9 ms): 32 x 32 matrix products 29.3, four waves
 // of 128 x 128 33.7 (registers spilled), k-tiles of 64 bytes in a ring of four or
-// five 28.3, raised wave priority around the products 30.1, other orders of the tiles
-// the same. With every operand in the nearest cache (not a right result) it takes
+// five 28.3, raised wave priority around the products 30.1, a workgroup that stays and
+// loads its next tile during a tile's end 27.5 (26.4 beside it), other orders of the
+// tiles the same. With every operand in the nearest cache (not a right result) it takes
 // 24.8: what memory costs.
 #pragma once
 
