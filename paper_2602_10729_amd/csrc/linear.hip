@@ -52,6 +52,12 @@ int64_t tiles_of(TileShape t, int64_t M, int64_t N) {
   return up(M, tile_m(t)) / tile_m(t) * (up(N, tile_n(t)) / tile_n(t));
 }
 
+// Few tokens: what takes the time is the matrix, not the products, and their errors
+// do not average out over many rows. Up to so many, logits go by small tiles, and d
+// is held in two 16-bit parts, as twice the tokens (128 x 32000 x 4096 bf16: 289
+// against 242 us; 16 x 32000 x 4096: 213 against 204).
+constexpr int64_t kFewTokens = 128;
+
 // The shape of the tiles and the splits of k that should take the least time: whole
 // rounds of workgroups, and for split sums their way through memory (4 bytes a
 // picosecond). A k-tile of as many tiles as a compute unit holds at once takes, in
@@ -61,13 +67,16 @@ struct Choice {
   TileShape tile;
   int64_t splits;
 };
-Choice choose(int type, int64_t M, int64_t N, int64_t k_tiles, int64_t most_splits) {
-  Choice best{kBig, 1};
+// `exact`: small tiles, which carry their sums on two levels (in fp32 these take 1.09
+// to 1.14 times as long over many tokens).
+Choice choose(int type, int64_t M, int64_t N, int64_t k_tiles, int64_t most_splits, bool exact) {
+  Choice best{exact ? kSmall : kBig, 1};
   double least = 1e300;
   for (const TileShape t : {kBig, kMiddle, kSmall}) {
+    if (exact && t != kSmall) continue;
     const int64_t tiles = tiles_of(t, M, N), at_once = kUnits * tile_at_once(t);
     const double k_tile = kTileTime[type == BO_TYPE_F32][t];
-    if (t != kBig && tiles * most_splits >= (int64_t)1 << 24) continue;      // (a launch's threads)
+    if (t != kBig && !exact && tiles * most_splits >= (int64_t)1 << 24) continue;      // (a launch's threads)
     for (int64_t s = 1; s <= most_splits && (s == 1 || s <= k_tiles / 8); ++s) {
       const double rounds = static_cast<double>((tiles * s + at_once - 1) / at_once);
       const double sums = s == 1 ? 0.0 : 5.0 + 2e-6 * static_cast<double>(s * M) * static_cast<double>(N);
@@ -85,7 +94,7 @@ struct Forward {
 };
 Forward forward_plan(const Shape& s) {
   Forward f;
-  f.tile = s.T <= 32 ? kNarrow32 : s.T <= 64 ? kNarrow64 : choose(s.type, s.V, s.T, 1, 1).tile;
+  f.tile = s.T <= 32 ? kNarrow32 : s.T <= 64 ? kNarrow64 : choose(s.type, s.V, s.T, 1, 1, s.T <= kFewTokens).tile;
   f.slots = up(s.V, tile_m(f.tile)) / tile_m(f.tile);
   int64_t at = 0;
   const auto take = [&](int64_t bytes) { const int64_t o = at; at += up(bytes, 256); return o; };
@@ -96,12 +105,6 @@ Forward forward_plan(const Shape& s) {
   f.total = at;
   return f;
 }
-
-// Up to so many tokens d is held in two 16-bit parts, as twice the tokens: over
-// few rows the rounding of their largest d does not average out, and their
-// products are not what takes the time (128 x 32000 x 4096 bf16: 289 against 242 us;
-// 16 x 32000 x 4096: 213 against 204).
-constexpr int64_t kFewTokens = 128;
 
 struct Backward {
   int64_t parts;                          // of d: 1 or 2
@@ -118,8 +121,10 @@ Backward backward_plan(const Shape& s) {
   b.piece = most < 256 ? 256 : most < all ? most : all;
   b.pieces = (all + b.piece - 1) / b.piece;
   const int64_t kK = 128 / s.es;
-  b.derivs = choose(s.type, b.piece, s.T, 1, 1).tile;
-  const Choice h = choose(s.type, s.H, T, b.piece / kK, 16), w = choose(s.type, s.H, b.piece, up(T, kK) / kK, 16);
+  const bool few = s.T <= kFewTokens;
+  b.derivs = choose(s.type, b.piece, s.T, 1, 1, few).tile;
+  const Choice h = choose(s.type, s.H, T, b.piece / kK, 16, few && b.parts == 1),
+               w = choose(s.type, s.H, b.piece, up(T, kK) / kK, 16, false);
   b.rows = h.tile;
   b.h_splits = h.splits;
   b.weight = w.tile;
