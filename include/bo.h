@@ -724,7 +724,7 @@ bo_status bo_dispatch(const int32_t* ids, int64_t N, int32_t E, int64_t capacity
  *          bo_linear_logprobs_workspace(..) bytes for these matrices;
  *          overwritten; calls that may overlap need one each. Rows that are
  *          not aligned to 4 bytes are copied into it first.
- * T >= 0 (0 is a no-op), T < 2^31, 1 <= V <= 2^29, T V <= 2^38,
+ * T >= 0 (0 is a no-op), T <= 2^28, 1 <= V <= 2^29, T V <= 2^38,
  * 1 <= H <= BO_MAX_WIDTH.
  * Asynchronous. Errors: INVALID_ARGUMENT, CAPACITY, DEVICE.
  */
@@ -748,7 +748,9 @@ bo_status bo_linear_logprobs(const void* hidden, int64_t hidden_stride, const vo
  * g_t counts as 0 in a row without a token. A row whose g_t and g_H are both 0
  * has gradient 0 and adds nothing to the matrix's, whatever it holds; any other
  * row with NaN stats, or a token >= V, makes its own gradient and the matrix's
- * NaN.
+ * NaN. A row without a distribution (every logit -inf) has gradient 0 too. An
+ * infinite or NaN element of the matrix makes its column of grad_hidden NaN in
+ * every row that has a gradient, also where it only masks: 0 times it is NaN.
  *
  * The logits are formed again, in pieces of the vocabulary. For 16-bit types a
  * piece of d is held in that type (f16: scaled by a power of two for the whole

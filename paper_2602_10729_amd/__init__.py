@@ -813,6 +813,7 @@ def _places(order, position, rows=None):
 def _out_rows(out, like, kind, stream, R, H):
     if out is None:
         out, = _new(like, stream, ((R, H), like.dtype))
+        return out, out.data_ptr(), H
     op, okind, oR, oH, ostride = _rows(out, "out")
     if (okind, oR, oH) != (kind, R, H):
         raise ValueError(f"out must have shape {(R, H)} and the input's type")

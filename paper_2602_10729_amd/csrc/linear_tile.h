@@ -91,7 +91,6 @@ namespace tile {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
@@ -111,18 +110,18 @@ __device__ __forceinline__ void load_lds(u32x4 buffer, const uint32_t (&offset)[
   static_assert(N == 1 || N == 2 || N == 4, "loads of a wave");
   if constexpr (N == 1) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-                 :: "s"(to), "v"(offset[0]), "s"(buffer) : "memory");
+                 :: "s"(to), "v"(offset[0]), "s"(buffer) : "memory", "m0");
   } else if constexpr (N == 2) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %2, %4, 0 offen lds\n\t"
                  "s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %3, %4, 0 offen lds"
-                 :: "s"(to), "s"(to + 1024), "v"(offset[0]), "v"(offset[1]), "s"(buffer) : "memory");
+                 :: "s"(to), "s"(to + 1024), "v"(offset[0]), "v"(offset[1]), "s"(buffer) : "memory", "m0");
   } else {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %4, %8, 0 offen lds\n\t"
                  "s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %5, %8, 0 offen lds\n\t"
                  "s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %6, %8, 0 offen lds\n\t"
                  "s_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %7, %8, 0 offen lds"
-                 :: "s"(to), "s"(to + 1024), "s"(to + 2048), "s"(to + 3072), "v"(offset[0]), "v"(offset[1]),
-                    "v"(offset[2]), "v"(offset[3]), "s"(buffer) : "memory");
+                 :: "s"(to), "s"(to + 1024), "s"(to + 2048), "s"(to + 3 * 1024), "v"(offset[0]), "v"(offset[1]),
+                    "v"(offset[2]), "v"(offset[3]), "s"(buffer) : "memory", "m0");
   }
 }
 

@@ -142,7 +142,7 @@ bo_status check_linear_sizes(int32_t type, int64_t T, int64_t V, int64_t H, floa
   if (T < 0 || V < 1 || H < 1) return fail(BO_ERR_INVALID_ARGUMENT, W + ": T < 0, V < 1 or H < 1");
   if (!(it > 0.0f) || !(it <= 1e30f))
     return fail(BO_ERR_INVALID_ARGUMENT, W + ": inv_temperature must be in (0, 1e30]");
-  if (T >= kMaxElems || V > kMaxElems / 4 || T > kMaxScores / V)
+  if (T > kMaxElems / 8 || V > kMaxElems / 4 || T > kMaxScores / V)
     return fail(BO_ERR_CAPACITY, W + ": T, V or T times V beyond limit");
   if (H > BO_MAX_WIDTH) return fail(BO_ERR_CAPACITY, W + ": H beyond BO_MAX_WIDTH");
   return BO_OK;

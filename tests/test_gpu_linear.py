@@ -308,6 +308,33 @@ def test_infinite_logits():
     assert not g.hidden.any() and not g.weight.any()
 
 
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("T", [1, 40, 300])
+def test_gradients_beside_masked_words(T, kind):
+    """Words masked by a matrix of minus infinity get no gradient and change no
+    other word's; the column that masks has none in the hidden rows."""
+    import torch
+    import paper_2602_10729_amd as bo
+    _announce("linear masked words", T, kind)
+    V, H, n = 700, 40, 30                    # the last n words are masked
+    h, w, tok, gl, gh = _inputs(T, V, H, kind, 17)
+    h[:, 0], tok[tok >= V - n] = 1.0, 5
+    w[V - n:, 0] = -INF
+    gl[T // 2:T // 2 + 3 * (T > 1)] = 0.0    # rows without a gradient, but for T = 1
+    gh[T // 2:T // 2 + 3 * (T > 1)] = 0.0
+    ref = Reference(h, w[:V - n], tok, 1.0)
+    r = bo.linear_logprobs(h, w, tok)
+    ref.check(r)
+    g = bo.linear_logprobs_grad(h, w, tok, r.stats, r.entropy, gl, gh)
+    live = (torch.where(tok >= 0, gl, 0.0) != 0) | (gh != 0)
+    assert bool(g.hidden[live, 0].isnan().all()) and not g.hidden[~live].any()
+    assert not g.weight[V - n:].any()
+    kept = bo.linear_logprobs_grad(h, w[:V - n], tok, r.stats, r.entropy, gl, gh)
+    ref.check_grad(kept, gl, gh, kind)
+    g.hidden[:, 0] = kept.hidden[:, 0]
+    ref.check_grad(bo.LinearLogprobsGrad(g.hidden, g.weight[:V - n]), gl, gh, kind)
+
+
 def test_unequal_gradients_in_half_precision():
     """f16 shares one scale over the call: small rows beside large ones, large and
     tiny gradients as loss scaling gives them."""

@@ -28,9 +28,9 @@ def test_linear_refusals(L):
         assert call(it=it) == INVALID
     assert call(hs=7) == INVALID and call(hidden=None) == INVALID
     assert call(hidden=ctypes.c_void_p(0x1002)) == INVALID            # not aligned to fp32
-    assert call(H=(1 << 20) + 1, hs=1 << 21, ws=1 << 21) == CAPACITY and call(T=2 ** 31) == CAPACITY
+    assert call(H=(1 << 20) + 1, hs=1 << 21, ws=1 << 21) == CAPACITY and call(T=2 ** 28 + 1) == CAPACITY
     assert call(V=2 ** 29 + 1) == CAPACITY and call(T=2 ** 20, V=2 ** 19) == CAPACITY
-    assert call(T=2 ** 30, V=1, H=1 << 20, hs=2 ** 40) == CAPACITY    # the extent overflows
+    assert call(T=2 ** 28, V=1, H=1 << 20, hs=2 ** 40) == CAPACITY    # the extent overflows
     assert call(T=0, hidden=None) == 0
 
     def grad(type=0, T=2, V=10, H=8, it=1.0, hs=8, gw=None):
