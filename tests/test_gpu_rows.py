@@ -243,6 +243,27 @@ def test_embed_grad_long_runs(T, V, H):
     _close(g, want, steps * EPS * size + HALF_ULP["bf16"] * 1.01 * np.abs(want) + 1e-37, "grad")
 
 
+@pytest.mark.parametrize("T,V,H", [(9000, 1000, 12), (7001, 600_000, 3), (100, 1_500_000, 2), (30_011, 3_000_001, 1)])
+def test_embed_grad_sorts(T, V, H):
+    """The widest digits and three of them, by one workgroup and by many; whole
+    numbers, so that sums are exact, and every call gives the same bits."""
+    import torch
+    import paper_2602_10729_amd as bo
+    _announce("embed sorts", T, V, H)
+    rng = np.random.default_rng(T)
+    ids = rng.integers(0, V, T)
+    ids[::3] = rng.integers(max(0, V - 20), V + 3, len(ids[::3]))       # some runs, some outside
+    ids[::11], ids[-1] = -1, V - 1
+    grad = rng.integers(-8, 9, (T, H)).astype(np.float32)
+    want = np.zeros((V, H), np.float32)
+    inside = (ids >= 0) & (ids < V)
+    np.add.at(want, ids[inside], grad[inside])
+    g = bo.embed_grad(_i64(ids), torch.from_numpy(grad).cuda(), V)
+    assert torch.equal(g.cpu(), torch.from_numpy(want))
+    noise = torch.randn((T, H), device="cuda")
+    assert torch.equal(bo.embed_grad(_i64(ids), noise, V), bo.embed_grad(_i64(ids), noise, V))
+
+
 def test_wide_and_far_rows():
     """Offsets past 2^31 elements, and rows wider than a wave's sweep."""
     import torch
