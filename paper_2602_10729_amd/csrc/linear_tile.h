@@ -548,13 +548,16 @@ __global__ __launch_bounds__(64 * WM * WN) void k_tile(TileArgs p) {
         live = on && q.live;
         const float ref = q.m == -__builtin_huge_valf() ? 0.0f : q.m;
         const float ls = q.ls * 1.44269504f, hot = q.g * p.it * scale, g = -hot, gh = -(q.gh * p.it * scale);
+        // where a probability is 0: no product with what may be infinite (a masked
+        // logit's u, or a large gradient times it), NaN only as the gradients' own
+        const float own = fmaf(gh, q.entropy, g), none = own != own ? own : 0.0f;
 #pragma unroll
         for (int i = 0; i < MI; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const float u2 = fmaf(acc[i][j][e] - ref, p.c, -ls);
-            const float lin = fmaf(fmaxf(u2, -1e30f), 0.69314718f, q.entropy);      // (finite where p is 0)
-            acc[i][j][e] = __builtin_amdgcn_exp2f(u2) * fmaf(gh, lin, g);
+            const float u2 = fmaf(acc[i][j][e] - ref, p.c, -ls), y = __builtin_amdgcn_exp2f(u2);
+            const float d = y * fmaf(gh, fmaf(u2, 0.69314718f, q.entropy), g);
+            acc[i][j][e] = y == 0.0f ? none : d;
           }
         const int64_t tok = q.token - (p.m0 + mw);
         if (__ballot(q.token >= 0 && tok >= 0 && tok < MI * 16)) {

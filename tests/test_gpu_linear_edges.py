@@ -1,0 +1,112 @@
+"""Log probabilities from hidden rows and their gradients where values, sizes and
+arguments are at their limits, on the GPU against the definitions in 64 bits.
+
+Inputs are drawn on the CPU, so that what a test needs of them (a clear largest
+logit, say) holds on every device. Roundings are counted as in test_gpu_linear: eps =
+2^-24 for fp32 sums, n additions within (2 sqrt(n) + 4) eps of the sum of the terms'
+sizes; d once to a 16-bit type (twice, so squared, up to 128 rows), outputs once.
+"""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+INF = np.inf
+EPS = 2.0 ** -24
+HALF_ULP = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}
+TINY = {"f32": 1e-36, "bf16": 1e-36, "f16": 2.0 ** -24}
+KINDS = ["f32", "bf16", "f16"]
+
+
+def _announce(*a):
+    print("[case]", *a, flush=True)
+
+
+def _dtype(name):
+    import torch
+    return {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}[name]
+
+
+def _gen(seed):
+    import torch
+    g = torch.Generator()
+    g.manual_seed(seed)
+    return g
+
+
+def _close(got, want, tol, what):
+    import torch
+    half = got.dtype is torch.float16
+    got = got.double()
+    assert got.shape == want.shape, what
+    ok = (got == want) | (got.isnan() & want.isnan()) | ((got - want).abs() <= tol)
+    if half:                       # from 65520 on, the nearest f16 is infinity
+        ok |= got.isinf() & (got.sign() == want.sign()) & (want.abs() + tol >= 65520.0)
+    if not bool(ok.all()):
+        bad = ~ok
+        raise AssertionError((what, int(bad.sum()), got[bad][:4].tolist(), want[bad][:4].tolist(),
+                              tol.expand_as(want)[bad][:4].tolist(), bad.nonzero()[:4].tolist()))
+
+
+def _product_check(got, d, other, kind, T, what, extra=None):
+    """got = d @ other: d off by a relative step of its own and `extra`, the sum and
+    the output by their roundings."""
+    n = d.shape[1]
+    own = 16 * EPS + (0.0 if kind == "f32" else HALF_ULP[kind] ** (2 if T <= 128 else 1) * 1.01)
+    ref = d @ other
+    tol = (own + (2 * n ** 0.5 + 4) * EPS) * (d.abs() @ other.abs())
+    if extra is not None:
+        tol = tol + extra @ other.abs()
+    _close(got, ref, tol + HALF_ULP[kind] * 1.01 * (ref.abs() + tol) + TINY[kind], what)
+
+
+def clear_rows(T, V, H, kind, seed, masked=0):
+    """(hidden, weight, tokens, favourites) with logits that are whole numbers, exact
+    in any order of summation: every row's largest is its favourite's, alone. The last
+    `masked` words have logits of -inf; column 0 is what masks."""
+    import torch
+    g = _gen(seed)
+    n = V - masked
+    w = torch.randint(-1, 2, (V, H), generator=g).double()
+    w[:, 0] = 0.0
+    w[:, 1] = 1.0
+    fav = torch.randint(n, (T,), generator=g)
+    h = 2.0 * w[fav]
+    h[:, 0] = 1.0
+    x = h @ w[:n].T
+    best = x.topk(2, 1)
+    assert bool((best.values[:, 0] >= best.values[:, 1] + 1).all()) and bool((best.indices[:, 0] == fav).all())
+    w[n:, 0] = -INF
+    tok = torch.randint(n, (T,), generator=g)
+    return h.to(_dtype(kind)), w.to(_dtype(kind)), tok, fav
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("T", [1, 40, 300])
+@pytest.mark.parametrize("it,masked", [(1e9, 30), (1e20, 0), (1e20, 30)])
+def test_entropy_gradients_of_words_without_probability(T, kind, it, masked):
+    """Far logits under a large inverse temperature: the largest has probability 1,
+    all others 0, and words of probability 0 have no part in the entropy's gradient,
+    however large it is (0 times what passes fp32 is no number)."""
+    import torch
+    import paper_2602_10729_amd as bo
+    _announce("linear no probability", T, kind, it, masked)
+    V, H = 700, 40
+    h, w, tok, fav = (t.cuda() for t in clear_rows(T, V, H, kind, 5, masked))
+    it = float(np.float32(it))
+    r = bo.linear_logprobs(h, w, tok, inv_temperature=it)
+    assert not r.entropy.any() and not r.stats[:, 1].any()
+    g, gh = torch.randn(T, generator=_gen(6)).cuda() / it, torch.ones(T, device="cuda")
+    got = bo.linear_logprobs_grad(h, w, tok, r.stats, r.entropy, g, gh, inv_temperature=it)
+    d = torch.zeros((T, V), dtype=torch.float64, device="cuda")
+    rows = torch.arange(T, device="cuda")
+    d[rows, tok] += it * g.double()
+    d[rows, fav] -= it * g.double()
+    # (f16: a step of 2^-38 of what a gradient may be, log V + 1 times the entropy's)
+    extra = torch.full_like(d, 2.0 ** -38 * it * float((np.log(V) + 1) * gh[0] + g.abs().max()) if kind == "f16" else 0.0)
+    first, n = (1, V - masked) if masked else (0, V)
+    if masked:
+        assert bool(got.hidden[:, 0].isnan().all()) and not got.weight[n:].any()
+    kept = w.double()
+    kept[:, 0] = 0.0
+    _product_check(got.hidden[:, first:], d, kept[:, first:], kind, T, "grad hidden", extra)
+    _product_check(got.weight[:n], d.T[:n], h.double(), kind, T, "grad weight", extra.T[:n])
