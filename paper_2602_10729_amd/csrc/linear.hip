@@ -187,16 +187,18 @@ hipError_t copy_rows(const void* in, int64_t rows, int64_t copies, int64_t strid
 
 // A workgroup 2^log_n tokens, its other lanes over the slots: each takes every
 // so-many'th, then neighbours are joined. Maxima first, so that sums need one
-// reference.
+// reference. Many tokens take several launches, from n0 on each: a workgroup for every
+// 64 of 2^28 would be 2^32 threads, more than a launch has.
+constexpr int64_t kJoinTokens = (int64_t)1 << 27;       // of a launch
 __global__ __launch_bounds__(1024) void k_linear_join(const float* __restrict__ part, int64_t slots,
                                                       const float* __restrict__ given, int64_t T, int64_t V,
                                                       const int64_t* __restrict__ tokens, float it, float c,
-                                                      int log_n, float* __restrict__ logprob,
+                                                      int log_n, int64_t n0, float* __restrict__ logprob,
                                                       float* __restrict__ entropy, float* __restrict__ stats) {
   __shared__ float red[1024];
   __shared__ float red2[1024];
   const int tid = threadIdx.x, tokens_here = 1 << log_n, shares = 1024 >> log_n;
-  const int64_t n = (static_cast<int64_t>(blockIdx.x) << log_n) + (tid & (tokens_here - 1));
+  const int64_t n = n0 + (static_cast<int64_t>(blockIdx.x) << log_n) + (tid & (tokens_here - 1));
   const int share = tid >> log_n;
   const bool on = n < T;
   float m = -__builtin_huge_valf();
@@ -360,9 +362,12 @@ hipError_t launch_linear(const LinearArgs& a, hipStream_t st) {
   if ((e = product(kFormLogprobs, p, s.type, f.tile, st)) != hipSuccess) return e;
   int log_n = 0;
   while (log_n < 6 && ((int64_t)64 << log_n) < s.T) ++log_n;
-  const unsigned grid = static_cast<unsigned>((s.T + ((int64_t)1 << log_n) - 1) >> log_n);
-  k_linear_join<<<grid, 1024, 0, st>>>(p.part, f.slots, p.given, s.T, s.V, a.tokens, a.it, p.c, log_n,
-                                       a.logprob, a.entropy, a.stats);
+  for (int64_t n0 = 0; n0 < s.T; n0 += kJoinTokens) {
+    const int64_t n = s.T - n0 < kJoinTokens ? s.T - n0 : kJoinTokens;
+    const unsigned grid = static_cast<unsigned>((n + ((int64_t)1 << log_n) - 1) >> log_n);
+    k_linear_join<<<grid, 1024, 0, st>>>(p.part, f.slots, p.given, s.T, s.V, a.tokens, a.it, p.c, log_n, n0,
+                                         a.logprob, a.entropy, a.stats);
+  }
   return hipGetLastError();
 }
 

@@ -110,3 +110,32 @@ def test_entropy_gradients_of_words_without_probability(T, kind, it, masked):
     kept[:, 0] = 0.0
     _product_check(got.hidden[:, first:], d, kept[:, first:], kind, T, "grad hidden", extra)
     _product_check(got.weight[:n], d.T[:n], h.double(), kind, T, "grad weight", extra.T[:n])
+
+
+def test_most_tokens():
+    """As many tokens as are taken, 2^28: every launch of the call fits its limits."""
+    import torch
+    import paper_2602_10729_amd as bo
+    _announce("linear most tokens")
+    T, V, H = 2 ** 28, 4, 2
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    h = torch.empty((T, H), dtype=torch.float16, device="cuda").normal_(generator=g)
+    w = torch.randn((V, H), generator=g, device="cuda").half()
+    tok = torch.randint(-1, V, (T,), generator=g, device="cuda")
+    r = bo.linear_logprobs(h, w, tok)
+    torch.cuda.synchronize()
+    for a in range(0, T, 2 ** 24):
+        s = slice(a, a + 2 ** 24)
+        x = h[s].double() @ w.double().T
+        lsm = torch.log_softmax(x, 1)
+        has = tok[s] >= 0
+        lp = torch.where(has, lsm.gather(1, tok[s].clamp(min=0)[:, None])[:, 0], 0.0)
+        m = x.amax(1)
+        # the bounds of test_gpu_linear at H = 2 (a logit within 7 eps of its products'
+        # sizes) and V = 4 (a sum within 65 eps, an entropy of at most 1.4)
+        size = (h[s].double().abs() @ w.double().abs().T).amax(1)
+        _close(r.logprob[s], lp, EPS * (28 * size + 80 + 8 * lp.abs()), "logprob")
+        _close(r.entropy[s], -(lsm.exp() * lsm).sum(1), EPS * (40 * size + 704), "entropy")
+        _close(r.stats[s, 0], m, EPS * 8 * size, "max")
+        _close(r.stats[s, 1], torch.logsumexp(x, 1) - m, EPS * (21 * size + 80), "log sum")
