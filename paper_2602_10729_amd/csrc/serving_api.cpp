@@ -3,9 +3,11 @@
 #include <hip/hip_runtime.h>
 
 #include <cmath>
+#include <initializer_list>
 #include <string>
 
 #include "serving.h"
+#include "spans.h"
 
 namespace {
 
@@ -102,23 +104,18 @@ bo_status check_route_sizes(int32_t type, int64_t T, int32_t E, int32_t score, i
   return BO_OK;
 }
 
-// Whether two matrices of `type` share an element. Rows that alternate within
-// one stride (column ranges of one buffer) do not.
-bool overlap(const void* p, int64_t p_rows, int64_t p_stride, const void* q, int64_t q_rows,
-             int64_t q_stride, int64_t cols, int32_t type) {
-  if (!p || !q || p_rows == 0 || q_rows == 0) return false;
+// A matrix of `type`, for what may not share memory.
+bo::Span matrix(const void* p, int32_t type, int64_t rows, int64_t cols, int64_t stride) {
   const int64_t es = static_cast<int64_t>(bo::type_bytes(type));
-  uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
-  const uintptr_t ae = a + static_cast<uintptr_t>(span_bytes(p_rows, cols, p_stride, es));
-  const uintptr_t be = b + static_cast<uintptr_t>(span_bytes(q_rows, cols, q_stride, es));
-  if (a >= be || b >= ae) return false;
-  if (p_stride != q_stride || p_rows == 1 || q_rows == 1) return true;
-  const uintptr_t pitch = static_cast<uintptr_t>(p_stride * es), width = static_cast<uintptr_t>(cols * es);
-  const uintptr_t off = (a > b ? a - b : b - a) % pitch;
-  return off < width || pitch - off < width;
+  return {p, rows, cols * es, rows > 1 ? stride * es : 0};
 }
-bo_status no_overlap(bool bad, const char* where, const char* what) {
-  return bad ? fail(BO_ERR_INVALID_ARGUMENT, std::string(where) + ": " + what) : BO_OK;
+// An output lies apart from what the call reads and from its other outputs.
+bo_status check_apart(const bo::Span& out, std::initializer_list<bo::Span> others, const char* where,
+                      const char* name) {
+  for (const bo::Span& o : others)
+    if (bo::share(out, o))
+      return fail(BO_ERR_INVALID_ARGUMENT, std::string(where) + ": " + name + " overlaps an input or another output");
+  return BO_OK;
 }
 
 constexpr int64_t kMaxPairs = ((int64_t)1 << 31) - 65536;
@@ -336,7 +333,7 @@ bo_status bo_expert_gather(const void* x, int32_t type, int64_t T, int64_t H, in
     if (T == 0 || R == 0) return BO_OK;
     if ((s = check_rows(x, type, T, H, stride, W, "x")) != BO_OK) return s;
     if ((s = check_rows(out, type, R, H, out_stride, W, "out")) != BO_OK) return s;
-    if ((s = no_overlap(overlap(x, T, stride, out, R, out_stride, H, type), W, "out overlaps x")) != BO_OK)
+    if ((s = check_apart(matrix(out, type, R, H, out_stride), {matrix(x, type, T, H, stride)}, W, "out")) != BO_OK)
       return s;
     if ((s = check_dev(order, 4 * static_cast<size_t>(R), "order")) != BO_OK) return s;
     if ((s = check_dev(position, 4 * static_cast<size_t>(T) * top, "position")) != BO_OK) return s;
@@ -357,7 +354,7 @@ bo_status bo_expert_combine(const void* rows, int32_t type, int64_t R, int64_t H
     if (T == 0) return BO_OK;
     if (R > 0 && (s = check_rows(rows, type, R, H, stride, W, "rows")) != BO_OK) return s;
     if ((s = check_rows(out, type, T, H, out_stride, W, "out")) != BO_OK) return s;
-    if ((s = no_overlap(overlap(rows, R, stride, out, T, out_stride, H, type), W, "out overlaps rows")) != BO_OK)
+    if ((s = check_apart(matrix(out, type, T, H, out_stride), {matrix(rows, type, R, H, stride)}, W, "out")) != BO_OK)
       return s;
     const size_t n = static_cast<size_t>(T) * top;
     if ((s = check_dev(position, 4 * n, "position")) != BO_OK) return s;
@@ -384,9 +381,9 @@ bo_status bo_expert_combine_grad(const void* grad, int32_t type, int64_t T, int6
     const size_t n = static_cast<size_t>(T) * top;
     if (grad_rows && R > 0) {
       if ((s = check_rows(grad_rows, type, R, H, grad_rows_stride, W, "grad_rows")) != BO_OK) return s;
-      if ((s = no_overlap(overlap(grad, T, grad_stride, grad_rows, R, grad_rows_stride, H, type) ||
-                          (grad_weights && overlap(rows, R, stride, grad_rows, R, grad_rows_stride, H, type)),
-                          W, "grad_rows overlaps an input")) != BO_OK)
+      if ((s = check_apart(matrix(grad_rows, type, R, H, grad_rows_stride),
+                           {matrix(grad, type, T, H, grad_stride), matrix(grad_weights ? rows : nullptr, type, R, H, stride)},
+                           W, "grad_rows")) != BO_OK)
         return s;
       if ((s = check_dev(order, 4 * static_cast<size_t>(R), "order")) != BO_OK) return s;
     }
@@ -411,7 +408,7 @@ bo_status bo_embed(const int64_t* tokens, int64_t T, const void* table, int32_t 
     if ((s = check_dev(tokens, 8 * static_cast<size_t>(T), "tokens")) != BO_OK) return s;
     if ((s = check_rows(table, type, V, H, stride, W, "table")) != BO_OK) return s;
     if ((s = check_rows(out, type, T, H, out_stride, W, "out")) != BO_OK) return s;
-    if ((s = no_overlap(overlap(table, V, stride, out, T, out_stride, H, type), W, "out overlaps table")) != BO_OK)
+    if ((s = check_apart(matrix(out, type, T, H, out_stride), {matrix(table, type, V, H, stride)}, W, "out")) != BO_OK)
       return s;
     bo::EmbedArgs a{tokens, table, type, T, V, H, stride, scale, out, out_stride, nullptr};
     hipStream_t st = static_cast<hipStream_t>(stream);
@@ -436,8 +433,8 @@ bo_status bo_embed_grad(const int64_t* tokens, int64_t T, const void* grad, int3
     if (T > 0) {
       if ((s = check_dev(tokens, 8 * static_cast<size_t>(T), "tokens")) != BO_OK) return s;
       if ((s = check_rows(grad, type, T, H, stride, W, "grad")) != BO_OK) return s;
-      if ((s = no_overlap(overlap(grad, T, stride, grad_table, V, grad_table_stride, H, type), W,
-                          "grad_table overlaps grad")) != BO_OK)
+      if ((s = check_apart(matrix(grad_table, type, V, H, grad_table_stride), {matrix(grad, type, T, H, stride)}, W,
+                           "grad_table")) != BO_OK)
         return s;
       if ((s = check_workspace(workspace, workspace_bytes, bo::embed_grad_workspace(T, V, H), W)) != BO_OK)
         return s;
@@ -522,13 +519,11 @@ bo_status bo_linear_logprobs_grad(const void* hidden, int64_t hidden_stride, con
       if ((s = check_dev(entropy, 4 * n, "entropy")) != BO_OK) return s;
       if (grad_logprob && (s = check_dev(grad_logprob, 4 * n, "grad_logprob")) != BO_OK) return s;
       if (grad_entropy && (s = check_dev(grad_entropy, 4 * n, "grad_entropy")) != BO_OK) return s;
-      if ((s = no_overlap(overlap(grad_hidden, T, grad_hidden_stride, hidden, T, hidden_stride, H, type) ||
-                          overlap(grad_hidden, T, grad_hidden_stride, weight, V, weight_stride, H, type) ||
-                          overlap(grad_weight, V, grad_weight_stride, hidden, T, hidden_stride, H, type) ||
-                          overlap(grad_weight, V, grad_weight_stride, weight, V, weight_stride, H, type) ||
-                          overlap(grad_hidden, T, grad_hidden_stride, grad_weight, V, grad_weight_stride, H, type),
-                          W, "a gradient overlaps an input or the other gradient")) != BO_OK)
-        return s;
+      const bo::Span gh = matrix(grad_hidden, type, T, H, grad_hidden_stride);
+      const bo::Span gw = matrix(grad_weight, type, V, H, grad_weight_stride);
+      const bo::Span in_h = matrix(hidden, type, T, H, hidden_stride), in_w = matrix(weight, type, V, H, weight_stride);
+      if ((s = check_apart(gh, {in_h, in_w, gw}, W, "grad_hidden")) != BO_OK) return s;
+      if ((s = check_apart(gw, {in_h, in_w}, W, "grad_weight")) != BO_OK) return s;
       if ((s = check_workspace(workspace, workspace_bytes, bo::linear_grad_workspace(a), W)) != BO_OK) return s;
     }
     hipStream_t st = static_cast<hipStream_t>(stream);
