@@ -719,7 +719,8 @@ bo_status bo_dispatch(const int32_t* ids, int64_t N, int32_t E, int64_t capacity
  *          both aligned to their type, strides >= H (any when one row)
  * tokens   device int64 [T], or NULL: no row has a token
  * inv_temperature  in (0, 1e30]
- * logprob, entropy device [T] out; stats device [T][2] out
+ * logprob, entropy device [T] out; stats device [T][2] out; none may overlap an
+ *          input or another
  * workspace  device, aligned to 16 bytes, of at least
  *          bo_linear_logprobs_workspace(..) bytes for these matrices;
  *          overwritten; calls that may overlap need one each. Rows that are
@@ -790,7 +791,7 @@ bo_status bo_linear_logprobs_grad(const void* hidden, int64_t hidden_stride, con
  *          T top when all are). A position outside [0, R) stands for none; the
  *          others are distinct, and order[position[p]] = p.
  * out      device [R][out_stride] of `type` out; outputs of these calls may
- *          not overlap their inputs
+ *          not overlap what they read or each other
  * top      1..BO_MAX_CHOICES; H >= 1; T top < 2^31 - 65536
  * Asynchronous. Errors: INVALID_ARGUMENT, CAPACITY, DEVICE.
  */
@@ -839,7 +840,7 @@ bo_status bo_expert_combine_grad(const void* grad, int32_t type, int64_t T, int6
  * stands for none: a row of 0; a token >= V gives a row of NaN.
  *
  * tokens device int64 [T]; table device [V][stride] of `type`, the first H of
- * each row used; out device [T][out_stride] of `type` out, may not overlap table
+ * each row used; out device [T][out_stride] of `type` out, may not overlap an input
  * 1 <= V < 2^31, H >= 1, 0 <= T < 2^31 - 65536; scale finite
  * Asynchronous. Errors: INVALID_ARGUMENT, CAPACITY, DEVICE.
  */
@@ -855,7 +856,7 @@ bo_status bo_embed(const int64_t* tokens, int64_t T, const void* table, int32_t 
  * and their rows of grad are not read.
  *
  * grad device [T][stride] of `type`; grad_table device [V][grad_table_stride] of
- * `type` out, may not overlap grad
+ * `type` out, may not overlap an input
  * workspace  device, aligned to 16 bytes, of bo_embed_grad_workspace(T, V, H)
  *        bytes (NULL when that is 0); overwritten; calls that may overlap need
  *        one each

@@ -109,6 +109,8 @@ bo::Span matrix(const void* p, int32_t type, int64_t rows, int64_t cols, int64_t
   const int64_t es = static_cast<int64_t>(bo::type_bytes(type));
   return {p, rows, cols * es, rows > 1 ? stride * es : 0};
 }
+// `n` elements of `es` bytes beside each other.
+bo::Span vec(const void* p, size_t n, size_t es = 4) { return {p, 1, static_cast<int64_t>(n * es), 0}; }
 // An output lies apart from what the call reads and from its other outputs.
 bo_status check_apart(const bo::Span& out, std::initializer_list<bo::Span> others, const char* where,
                       const char* name) {
@@ -333,10 +335,12 @@ bo_status bo_expert_gather(const void* x, int32_t type, int64_t T, int64_t H, in
     if (T == 0 || R == 0) return BO_OK;
     if ((s = check_rows(x, type, T, H, stride, W, "x")) != BO_OK) return s;
     if ((s = check_rows(out, type, R, H, out_stride, W, "out")) != BO_OK) return s;
-    if ((s = check_apart(matrix(out, type, R, H, out_stride), {matrix(x, type, T, H, stride)}, W, "out")) != BO_OK)
+    const size_t n = static_cast<size_t>(T) * top, r = static_cast<size_t>(R);
+    if ((s = check_dev(order, 4 * r, "order")) != BO_OK) return s;
+    if ((s = check_dev(position, 4 * n, "position")) != BO_OK) return s;
+    if ((s = check_apart(matrix(out, type, R, H, out_stride),
+                         {matrix(x, type, T, H, stride), vec(order, r), vec(position, n)}, W, "out")) != BO_OK)
       return s;
-    if ((s = check_dev(order, 4 * static_cast<size_t>(R), "order")) != BO_OK) return s;
-    if ((s = check_dev(position, 4 * static_cast<size_t>(T) * top, "position")) != BO_OK) return s;
     bo::ExpertArgs a{x, nullptr, type, T, H, R, stride, 0, top, order, position, nullptr, out,
                      out_stride, nullptr};
     hipStream_t st = static_cast<hipStream_t>(stream);
@@ -354,11 +358,12 @@ bo_status bo_expert_combine(const void* rows, int32_t type, int64_t R, int64_t H
     if (T == 0) return BO_OK;
     if (R > 0 && (s = check_rows(rows, type, R, H, stride, W, "rows")) != BO_OK) return s;
     if ((s = check_rows(out, type, T, H, out_stride, W, "out")) != BO_OK) return s;
-    if ((s = check_apart(matrix(out, type, T, H, out_stride), {matrix(rows, type, R, H, stride)}, W, "out")) != BO_OK)
-      return s;
     const size_t n = static_cast<size_t>(T) * top;
     if ((s = check_dev(position, 4 * n, "position")) != BO_OK) return s;
     if (weights && (s = check_dev(weights, 4 * n, "weights")) != BO_OK) return s;
+    if ((s = check_apart(matrix(out, type, T, H, out_stride),
+                         {matrix(rows, type, R, H, stride), vec(position, n), vec(weights, n)}, W, "out")) != BO_OK)
+      return s;
     bo::ExpertArgs a{nullptr, rows, type, T, H, R, 0, stride, top, nullptr, position, weights, out,
                      out_stride, nullptr};
     hipStream_t st = static_cast<hipStream_t>(stream);
@@ -378,18 +383,20 @@ bo_status bo_expert_combine_grad(const void* grad, int32_t type, int64_t T, int6
     if (T == 0) return BO_OK;
     if ((s = check_rows(grad, type, T, H, grad_stride, W, "grad")) != BO_OK) return s;
     if (grad_weights && R > 0 && (s = check_rows(rows, type, R, H, stride, W, "rows")) != BO_OK) return s;
-    const size_t n = static_cast<size_t>(T) * top;
+    const size_t n = static_cast<size_t>(T) * top, r = static_cast<size_t>(R);
     if (grad_rows && R > 0) {
       if ((s = check_rows(grad_rows, type, R, H, grad_rows_stride, W, "grad_rows")) != BO_OK) return s;
-      if ((s = check_apart(matrix(grad_rows, type, R, H, grad_rows_stride),
-                           {matrix(grad, type, T, H, grad_stride), matrix(grad_weights ? rows : nullptr, type, R, H, stride)},
-                           W, "grad_rows")) != BO_OK)
-        return s;
-      if ((s = check_dev(order, 4 * static_cast<size_t>(R), "order")) != BO_OK) return s;
+      if ((s = check_dev(order, 4 * r, "order")) != BO_OK) return s;
     }
     if ((s = check_dev(position, 4 * n, "position")) != BO_OK) return s;
     if (weights && (s = check_dev(weights, 4 * n, "weights")) != BO_OK) return s;
     if (grad_weights && (s = check_dev(grad_weights, 4 * n, "grad_weights")) != BO_OK) return s;
+    const bo::Span gr = matrix(grad_rows, type, R, H, grad_rows_stride), gw = vec(grad_weights, n);
+    const bo::Span in_g = matrix(grad, type, T, H, grad_stride);
+    const bo::Span in_r = matrix(grad_weights ? rows : nullptr, type, R, H, stride);      // (else not read)
+    const bo::Span in_o = vec(grad_rows ? order : nullptr, r), in_p = vec(position, n), in_w = vec(weights, n);
+    if ((s = check_apart(gr, {in_g, in_r, in_o, in_p, in_w, gw}, W, "grad_rows")) != BO_OK) return s;
+    if ((s = check_apart(gw, {in_g, in_r, in_o, in_p, in_w}, W, "grad_weights")) != BO_OK) return s;
     bo::ExpertArgs a{grad, rows, type, T, H, R, grad_stride, stride, top, order, position, weights,
                      R > 0 ? grad_rows : nullptr, grad_rows_stride, grad_weights};
     hipStream_t st = static_cast<hipStream_t>(stream);
@@ -408,7 +415,8 @@ bo_status bo_embed(const int64_t* tokens, int64_t T, const void* table, int32_t 
     if ((s = check_dev(tokens, 8 * static_cast<size_t>(T), "tokens")) != BO_OK) return s;
     if ((s = check_rows(table, type, V, H, stride, W, "table")) != BO_OK) return s;
     if ((s = check_rows(out, type, T, H, out_stride, W, "out")) != BO_OK) return s;
-    if ((s = check_apart(matrix(out, type, T, H, out_stride), {matrix(table, type, V, H, stride)}, W, "out")) != BO_OK)
+    if ((s = check_apart(matrix(out, type, T, H, out_stride),
+                         {matrix(table, type, V, H, stride), vec(tokens, static_cast<size_t>(T), 8)}, W, "out")) != BO_OK)
       return s;
     bo::EmbedArgs a{tokens, table, type, T, V, H, stride, scale, out, out_stride, nullptr};
     hipStream_t st = static_cast<hipStream_t>(stream);
@@ -433,7 +441,8 @@ bo_status bo_embed_grad(const int64_t* tokens, int64_t T, const void* grad, int3
     if (T > 0) {
       if ((s = check_dev(tokens, 8 * static_cast<size_t>(T), "tokens")) != BO_OK) return s;
       if ((s = check_rows(grad, type, T, H, stride, W, "grad")) != BO_OK) return s;
-      if ((s = check_apart(matrix(grad_table, type, V, H, grad_table_stride), {matrix(grad, type, T, H, stride)}, W,
+      if ((s = check_apart(matrix(grad_table, type, V, H, grad_table_stride),
+                           {matrix(grad, type, T, H, stride), vec(tokens, static_cast<size_t>(T), 8)}, W,
                            "grad_table")) != BO_OK)
         return s;
       if ((s = check_workspace(workspace, workspace_bytes, bo::embed_grad_workspace(T, V, H), W)) != BO_OK)
@@ -469,6 +478,11 @@ bo_status bo_linear_logprobs(const void* hidden, int64_t hidden_stride, const vo
     if ((s = check_dev(logprob, 4 * n, "logprob")) != BO_OK) return s;
     if ((s = check_dev(entropy, 4 * n, "entropy")) != BO_OK) return s;
     if ((s = check_dev(stats, 8 * n, "stats")) != BO_OK) return s;
+    const bo::Span in_h = matrix(hidden, type, T, H, hidden_stride), in_w = matrix(weight, type, V, H, weight_stride);
+    const bo::Span in_t = vec(tokens, n, 8), lp = vec(logprob, n), en = vec(entropy, n), sm = vec(stats, 2 * n);
+    if ((s = check_apart(lp, {in_h, in_w, in_t, en, sm}, W, "logprob")) != BO_OK) return s;
+    if ((s = check_apart(en, {in_h, in_w, in_t, sm}, W, "entropy")) != BO_OK) return s;
+    if ((s = check_apart(sm, {in_h, in_w, in_t}, W, "stats")) != BO_OK) return s;
     bo::LinearArgs a = linear_args(hidden, hidden_stride, weight, weight_stride, type, T, V, H);
     if ((s = check_workspace(workspace, workspace_bytes, bo::linear_workspace(a), W)) != BO_OK) return s;
     a.tokens = tokens; a.it = inv_temperature;
@@ -522,8 +536,10 @@ bo_status bo_linear_logprobs_grad(const void* hidden, int64_t hidden_stride, con
       const bo::Span gh = matrix(grad_hidden, type, T, H, grad_hidden_stride);
       const bo::Span gw = matrix(grad_weight, type, V, H, grad_weight_stride);
       const bo::Span in_h = matrix(hidden, type, T, H, hidden_stride), in_w = matrix(weight, type, V, H, weight_stride);
-      if ((s = check_apart(gh, {in_h, in_w, gw}, W, "grad_hidden")) != BO_OK) return s;
-      if ((s = check_apart(gw, {in_h, in_w}, W, "grad_weight")) != BO_OK) return s;
+      const bo::Span in_t = vec(tokens, n, 8), in_s = vec(stats, 2 * n), in_e = vec(entropy, n);
+      const bo::Span in_gl = vec(grad_logprob, n), in_ge = vec(grad_entropy, n);
+      if ((s = check_apart(gh, {in_h, in_w, in_t, in_s, in_e, in_gl, in_ge, gw}, W, "grad_hidden")) != BO_OK) return s;
+      if ((s = check_apart(gw, {in_h, in_w, in_t, in_s, in_e, in_gl, in_ge}, W, "grad_weight")) != BO_OK) return s;
       if ((s = check_workspace(workspace, workspace_bytes, bo::linear_grad_workspace(a), W)) != BO_OK) return s;
     }
     hipStream_t st = static_cast<hipStream_t>(stream);

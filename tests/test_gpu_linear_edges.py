@@ -139,3 +139,49 @@ def test_most_tokens():
         _close(r.entropy[s], -(lsm.exp() * lsm).sum(1), EPS * (40 * size + 704), "entropy")
         _close(r.stats[s, 0], m, EPS * 8 * size, "max")
         _close(r.stats[s, 1], torch.logsumexp(x, 1) - m, EPS * (21 * size + 80), "log sum")
+
+
+def test_outputs_that_share_memory_are_refused():
+    import torch
+    import paper_2602_10729_amd as bo
+    _announce("linear overlaps")
+    T, V, H = 8, 100, 16
+    g = _gen(14)
+    h, w = torch.randn((T, H), generator=g).cuda(), torch.randn((V, H), generator=g).cuda()
+    tok = torch.randint(V, (T,), generator=g).cuda()
+    r = bo.linear_logprobs(h, w, tok)
+    lp, en, st = (torch.empty_like(t) for t in r)
+    gl, gh = torch.ones(T, device="cuda"), torch.ones(T, device="cuda")
+    words = tok.view(torch.float32)                  # the tokens' memory
+    grad = lambda out: bo.linear_logprobs_grad(h, w, tok, r.stats, r.entropy, gl, gh, out=out)
+    row = lambda t: t.view(T, 1)                     # a gradient of one column in a vector's place
+    h1, w1 = h[:, :1].contiguous(), w[:, :1].contiguous()
+    narrow = lambda out: bo.linear_logprobs_grad(h1, w1, tok, r.stats, r.entropy, gl, gh, out=out)
+    big = torch.empty(3 * T, device="cuda")
+    bad = [
+        lambda: bo.linear_logprobs(h, w, tok, out=(lp, lp, st)), lambda: bo.linear_logprobs(h, w, tok, out=(big[4:12], big[:8], st)),
+        lambda: bo.linear_logprobs(h, w, tok, out=(lp, big[:8], big[4:20].view(T, 2))),
+        lambda: bo.linear_logprobs(h, w, tok, out=(h.view(-1)[:T], en, st)), lambda: bo.linear_logprobs(h, w, tok, out=(lp, w[1, :8], st)),
+        lambda: bo.linear_logprobs(h, w, tok, out=(words[:T], en, st)), lambda: bo.linear_logprobs(h, w, tok, out=(lp, en, words.view(T, 2))),
+        lambda: narrow((row(gl), None)), lambda: narrow((row(gh), None)), lambda: narrow((row(r.entropy), None)),
+        lambda: narrow((r.stats[:, :1], None)), lambda: narrow((words[:T].view(T, 1), None)),
+    ]
+    keep = [t.clone() for t in (h, w, tok, *r, gl, gh)]
+    for i, f in enumerate(bad):
+        with pytest.raises(bo.BoError, match="overlap"):
+            f()
+            print("accepted", i, flush=True)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(keep, (h, w, tok, *r, gl, gh)))
+    # side by side, and vectors in the columns that a matrix leaves, share nothing
+    out = bo.linear_logprobs(h, w, tok, out=(big[:8], big[8:16], torch.empty_like(st)))
+    assert all(torch.equal(a, b) for a, b in zip(out, r))
+    wide = torch.zeros((V, H + 8), device="cuda")
+    wide[:, :H] = w
+    out = bo.linear_logprobs(h, wide[:, :H], tok, out=(wide[3, H:], wide[4, H:], st))
+    assert all(torch.equal(a, b) for a, b in zip(out, r)) and torch.equal(wide[:, :H], w)
+    both = torch.empty((T, 2 * H), device="cuda")
+    both[:, :H] = h
+    g1 = bo.linear_logprobs_grad(both[:, :H], w, tok, r.stats, r.entropy, gl, gh, out=(both[:, H:], torch.empty_like(w)))
+    g2 = bo.linear_logprobs_grad(h, w, tok, r.stats, r.entropy, gl, gh)
+    assert torch.equal(g1[0], g2.hidden) and torch.equal(g1[1], g2.weight)

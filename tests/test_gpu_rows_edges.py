@@ -85,3 +85,40 @@ def test_one_row_that_shares_memory_is_refused():
             print("accepted", i, flush=True)
     torch.cuda.synchronize()
     assert torch.equal(one, keep)
+
+
+def test_outputs_in_the_place_of_vectors_are_refused():
+    import torch
+    import paper_2602_10729_amd as bo
+    _announce("rows, vectors shared")
+    T, top, H = 4, 2, 16
+    x, rows = torch.ones((T, H), device="cuda"), torch.ones((T * top, H), device="cuda")
+    order = torch.arange(T * top, dtype=torch.int32, device="cuda")
+    position, w = order.view(T, top).clone(), torch.ones((T, top), device="cuda")
+    gw, tok = torch.empty_like(w), torch.zeros(T, dtype=torch.int64, device="cuda")
+    gx = torch.ones((T * top, H), device="cuda")
+    floats = lambda t: t.view(-1).view(torch.float32)
+    col = lambda t, n: floats(t)[:n].view(n, 1)      # a matrix of one column in its place
+    bad = [
+        lambda: bo.expert_gather(x[:, :1], order, position, out=col(order, 8)),
+        lambda: bo.expert_gather(x[:, :1], order, position, out=col(position, 8)),
+        lambda: bo.expert_combine(rows[:, :1], position, w, out=col(position, 4)),
+        lambda: bo.expert_combine(rows[:, :1], position, w, out=col(w, 4)),
+        lambda: bo.expert_combine_grad(x, rows, order, position, w, out=(gx, w)),
+        lambda: bo.expert_combine_grad(x, rows, order, position, w, out=(gx, floats(position).view(T, top))),
+        lambda: bo.expert_combine_grad(x, rows, order, position, w, out=(gx, rows[0, :8].view(T, top))),
+        lambda: bo.expert_combine_grad(x, rows, order, position, w, out=(gx, x[0, 4:12].view(T, top))),
+        lambda: bo.expert_combine_grad(x, rows, order, position, w, out=(gx, gx[7, 4:12].view(T, top))),
+        lambda: bo.expert_combine_grad(x[:, :1], rows[:, :1], order, position, w, out=(col(w, 8), gw)),
+        lambda: bo.expert_combine_grad(x[:, :1], rows[:, :1], order, position, w, out=(col(order, 8), gw)),
+        lambda: bo.expert_combine_grad(x[:, :1], rows[:, :1], order, position, w, out=(col(position, 8), None)),
+        lambda: bo.embed(tok, rows[:, :1], out=col(tok, 4)), lambda: bo.embed_grad(tok, x[:, :1], 3, out=col(tok, 3)),
+    ]
+    held = (x, rows, order, position, w, tok)
+    keep = [t.clone() for t in held]
+    for i, f in enumerate(bad):
+        with pytest.raises(bo.BoError, match="overlap"):
+            f()
+            print("accepted", i, flush=True)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(keep, held))
