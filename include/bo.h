@@ -754,10 +754,12 @@ bo_status bo_linear_logprobs(const void* hidden, int64_t hidden_stride, const vo
  * every row that has a gradient, also where it only masks: 0 times it is NaN.
  *
  * The logits are formed again, in pieces of the vocabulary. For 16-bit types a
- * piece of d is held in that type (f16: scaled by a power of two for the whole
- * call, so that its largest is near 2^14): one rounding of each d, which is of
- * the size of the outputs' own, and averages out over many rows; up to 128 rows
- * it is held in two such parts. Sums are fp32, and the outputs rounded once.
+ * piece of d is held in that type: one rounding of each d, which is of the size
+ * of the outputs' own, and averages out over many rows; up to 128 rows it is held
+ * in two such parts. f16 scales d by powers of two, so that its largest is near
+ * 2^14: on its way to grad_hidden each row by its own, on its way to grad_weight
+ * all rows by one, so that there d has a step of 2^-38 of the call's largest.
+ * Sums are fp32, and the outputs rounded once.
  *
  * stats, entropy: as bo_linear_logprobs returned them
  * grad_logprob, grad_entropy device [T], or NULL: 0

@@ -112,7 +112,7 @@ struct Backward {
   TileShape derivs, rows, weight;
   int64_t h_splits, w_splits;
   bool h_direct;
-  int64_t coef, largest, hidden, weight_copy, d, h_sums, w_sums, total;
+  int64_t coef, largest, hidden, weight_copy, d, d_rows, h_sums, w_sums, total;
 };
 Backward backward_plan(const Shape& s) {
   Backward b;
@@ -137,6 +137,7 @@ Backward backward_plan(const Shape& s) {
   b.hidden = take(T * s.Hp * s.es);
   b.weight_copy = take(s.copy_weight ? s.V * s.Hp * s.es : 0);
   b.d = take(T * b.piece * s.es);
+  b.d_rows = take(s.type == BO_TYPE_F16 ? T * b.piece * s.es : 0);
   b.h_sums = take(b.h_direct ? 0 : b.h_splits * T * s.Hp * 4);
   b.w_sums = take(b.w_splits == 1 ? 0 : b.w_splits * b.piece * s.Hp * 4);
   b.total = at;
@@ -270,11 +271,12 @@ __global__ __launch_bounds__(kWg) void k_linear_coef(const int64_t* __restrict__
     q.entropy = entropy[t];
     if (tok >= V && q.live) q.g = __builtin_nanf("");
     q.token = tok >= 0 && tok < V ? static_cast<int32_t>(tok) : -1;
-    q.pad = 0;
-    coef[t] = q;
-    // |p (u + H)| < H + 1 <= log V + 1
+    // |p (u + H)| < H + 1 <= log V + 1; what is no finite size scales nothing
     const float size = it * (fabsf(q.g) + (log_v + 1.0f) * fabsf(q.gh));
-    most = fmaxf(most, size);
+    const float bound = q.live && size < __builtin_huge_valf() ? size : 0.0f;
+    q.exponent = exponent_of(bound);
+    coef[t] = q;
+    most = fmaxf(most, bound);
   }
 #pragma unroll
   for (int off = 32; off; off >>= 1) most = fmaxf(most, __shfl_xor(most, off));
@@ -294,7 +296,7 @@ __global__ __launch_bounds__(kWg) void k_linear_round(const float* __restrict__ 
                                                       const TokenCoef* __restrict__ coef,
                                                       const float* __restrict__ largest,
                                                       typename Elem<TYPE>::T* __restrict__ out, int64_t stride) {
-  const float scale = TYPE == BO_TYPE_F16 ? exp2i(-deriv_exponent(largest)) : 1.0f;
+  const int common = TYPE == BO_TYPE_F16 ? common_exponent(largest) : 0;
   const int64_t per = Hp / 4, n = rows * per, all = static_cast<int64_t>(gridDim.x) * kWg;
   for (int64_t i = static_cast<int64_t>(blockIdx.x) * kWg + threadIdx.x; i < n; i += all) {
     const int64_t r = i / per, h = i % per * 4;
@@ -306,6 +308,7 @@ __global__ __launch_bounds__(kWg) void k_linear_round(const float* __restrict__ 
           const float4 o = *reinterpret_cast<const float4*>(sums + s * split_stride + (d * rows + r) * Hp + h);
           v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
         }
+    const float scale = TYPE == BO_TYPE_F16 ? exp2i(-(coef ? coef[r].exponent : common)) : 1.0f;
     const float f[4] = {v.x * scale, v.y * scale, v.z * scale, v.w * scale};
 #pragma unroll
     for (int e = 0; e < 4; ++e)
@@ -402,6 +405,9 @@ hipError_t launch_linear_grad(const LinearArgs& a, hipStream_t st) {
   float* h_sums = reinterpret_cast<float*>(w + b.h_sums);
   float* w_sums = reinterpret_cast<float*>(w + b.w_sums);
   const int64_t kK = 128 / s.es;
+  const bool scaled = s.type == BO_TYPE_F16;
+  char* d = w + b.d;                      // what grad_weight reads, and what grad_hidden does
+  char* d_rows = scaled ? w + b.d_rows : d;
   for (int64_t i = 0; i < b.pieces; ++i) {
     const int64_t v0 = i * b.piece, cols = s.V - v0 < b.piece ? s.V - v0 : b.piece;
     TileArgs p{};
@@ -414,12 +420,14 @@ hipError_t launch_linear_grad(const LinearArgs& a, hipStream_t st) {
     p.coef = coef; p.largest = largest;
     p.low = b.parts > 1;
     p.m0 = v0;
-    p.out = w + b.d; p.out_stride = b.piece;
+    p.out = scaled && !a.grad_weight ? nullptr : d;
+    p.out_rows = scaled && a.grad_hidden ? d_rows : nullptr;
+    p.out_stride = b.piece;
     if ((e = product(kFormDerivs, p, s.type, b.derivs, st)) != hipSuccess) return e;
     if (a.grad_hidden) {
       TileArgs q{};
       q.a = weight + v0 * weight_stride; q.a_stride = weight_stride;
-      q.b = w + b.d; q.b_stride = b.piece * s.es;
+      q.b = d_rows; q.b_stride = b.piece * s.es;
       q.M = s.H; q.N = b.parts * s.T; q.K = cols;
       q.splits = static_cast<int>(b.h_splits);
       q.split_k = (b.piece / kK + b.h_splits - 1) / b.h_splits;
@@ -436,7 +444,7 @@ hipError_t launch_linear_grad(const LinearArgs& a, hipStream_t st) {
     if (a.grad_weight) {
       TileArgs q{};
       q.a = hidden; q.a_stride = s.Hp * s.es;
-      q.b = w + b.d; q.b_stride = b.piece * s.es;
+      q.b = d; q.b_stride = b.piece * s.es;
       q.M = s.H; q.N = cols; q.K = b.parts * s.T;
       q.splits = static_cast<int>(b.w_splits);
       q.split_k = (up(b.parts * s.T, kK) / kK + b.w_splits - 1) / b.w_splits;

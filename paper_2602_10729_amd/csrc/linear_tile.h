@@ -45,7 +45,8 @@ enum Epilogue { kLogprobs, kDerivs, kSums, kRows };
 struct TokenCoef {
   float m, ls, g, gh, entropy;            // stats; the gradients that come in
   int32_t token;                          // or -1
-  int32_t live, pad;
+  int32_t live;
+  int32_t exponent;                       // of the power of two by which f16 multiplies its derivatives
 };
 
 struct TileArgs {
@@ -62,11 +63,12 @@ struct TileArgs {
   float* given;                           // [N]
   // kDerivs
   const TokenCoef* coef;                  // (kRows: of out's rows, or nullptr)
-  const float* largest;                   // [64], for the scale of f16
+  const float* largest;                   // [64], for the scale of f16 that all tokens share
   float it;
+  void* out_rows;                         // f16: under each token's own scale, or nullptr
   int low;                                // rows N + n: what the rounding of rows n left
   int64_t m0;                             // first m of the piece, in the vocabulary
-  // out
+  // out (kDerivs in f16: under the common scale, or nullptr)
   void* out;
   int64_t out_stride;                     // elements
   int64_t out_split;                      // elements between splits (kSums)
@@ -75,15 +77,19 @@ struct TileArgs {
 
 constexpr int kLargest = 64;              // partial maxima of the gradients
 
-// The power of two by which f16 derivatives are multiplied: the largest lies in
-// [2^13, 2^14] by its bound, so that sums of two stay finite.
-__device__ __forceinline__ int deriv_exponent(const float* largest) {
+// The power of two by which f16 derivatives of at most `bound` are multiplied: the
+// largest lies in [2^13, 2^14], so that sums of two stay finite.
+__device__ __forceinline__ int exponent_of(float bound) {
+  if (!(bound > 0.0f) || !(bound < __builtin_huge_valf())) return 0;
+  const int e = 13 - static_cast<int>((__float_as_uint(bound) >> 23) & 0xFF) + 127;
+  return e < -120 ? -120 : e > 120 ? 120 : e;
+}
+// That of all tokens, from partial maxima of their bounds.
+__device__ __forceinline__ int common_exponent(const float* largest) {
   float v = largest[threadIdx.x & 63];
 #pragma unroll
   for (int off = 32; off; off >>= 1) v = fmaxf(v, __shfl_xor(v, off));
-  if (!(v > 0.0f) || !(v < __builtin_huge_valf())) return 0;
-  const int e = 13 - static_cast<int>((__float_as_uint(v) >> 23) & 0xFF) + 127;
-  return e < -120 ? -120 : e > 120 ? 120 : e;
+  return exponent_of(v);
 }
 __device__ __forceinline__ float exp2i(int e) { return __uint_as_float(static_cast<unsigned>(e + 127) << 23); }
 
@@ -535,17 +541,24 @@ __global__ __launch_bounds__(64 * WM * WN) void k_tile(TileArgs p) {
     constexpr int kGranules = MI * 16 * static_cast<int>(sizeof(S)) / 16, kSwizzle = kGranules < 16 ? kGranules - 1 : 15;
     static_assert(kWaves * 16 * kGranules * 16 <= STAGES * kStage, "a block of every wave fits");
     char* mine = lds + wave * (16 * kGranules * 16);
-    float scale = 1.0f;
-    if constexpr (TYPE == BO_TYPE_F16 && EPI == kDerivs) scale = exp2i(deriv_exponent(p.largest));
-    if constexpr (TYPE == BO_TYPE_F16 && EPI == kRows) scale = exp2i(-deriv_exponent(p.largest));
+    // f16 derivatives are held twice: a token's sum over the vocabulary reads them under
+    // a scale of its own, a word's sum over the tokens under one that all share (3.84
+    // against 3.69 ms with that one alone at 8192 x 32000 x 2048, both gradients, where a
+    // token 2^26 below another's lost what the softmax subtracts).
+    constexpr int kScales = TYPE == BO_TYPE_F16 && EPI == kDerivs ? 2 : 1;
+    int common = 0;
+    if constexpr (TYPE == BO_TYPE_F16 && EPI != kSums) common = common_exponent(p.largest);
 #pragma unroll
     for (int j = 0; j < NI; ++j) {
       const int64_t n = nw + 16 * j + (lane & 15);
       const bool on = n < p.N;
       bool live = on;
+      float to_common = 1.0f;
       if constexpr (EPI == kDerivs) {
         const TokenCoef q = p.coef[on ? n : 0];
         live = on && q.live;
+        const float scale = kScales == 2 ? exp2i(q.exponent) : 1.0f;
+        if constexpr (kScales == 2) to_common = exp2i(max(common - q.exponent, -126));
         const float ref = q.m == -__builtin_huge_valf() ? 0.0f : q.m;
         const float ls = q.ls * 1.44269504f, hot = q.g * p.it * scale, g = -hot, gh = -(q.gh * p.it * scale);
         // where a probability is 0: no product with what may be infinite (a masked
@@ -577,6 +590,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_tile(TileArgs p) {
       if constexpr (EPI == kRows) {
         live = on && (!p.coef || p.coef[n].live);
         if constexpr (TYPE == BO_TYPE_F16) {
+          const float scale = exp2i(-(p.coef && on ? p.coef[n].exponent : common));
 #pragma unroll
           for (int i = 0; i < MI; ++i) acc[i][j] *= scale;
         }
@@ -587,21 +601,26 @@ __global__ __launch_bounds__(64 * WM * WN) void k_tile(TileArgs p) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) acc[i][j][e] = live ? acc[i][j][e] : 0.0f;
       }
+      // every scale's values, then (p.low) what their rounding left
       const int halves = EPI == kDerivs && TYPE != BO_TYPE_F32 && p.low ? 2 : 1;
-      for (int half = 0; half < halves; ++half) {
-        if (half) {                                // what the rounding left
-#pragma unroll
-          for (int i = 0; i < MI; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) acc[i][j][e] -= Elem<TYPE>::load(Elem<TYPE>::store(acc[i][j][e]));
-        }
+      for (int pass = 0; pass < kScales * halves; ++pass) {
+        const bool shared = kScales == 2 && pass >= halves;
+        const int half = shared ? pass - halves : pass;
+        S* base = static_cast<S*>(kScales == 2 && !shared ? p.out_rows : p.out);
+        if (kScales == 2 && !base) continue;
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
           S h[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            if constexpr (EPI == kSums) h[e] = acc[i][j][e];
-            else h[e] = Elem<TYPE>::store(acc[i][j][e]);
+            float v = acc[i][j][e];
+            if (shared) v *= to_common;
+            if constexpr (EPI == kSums) {
+              h[e] = v;
+            } else {
+              h[e] = Elem<TYPE>::store(v);
+              if (half) h[e] = Elem<TYPE>::store(v - Elem<TYPE>::load(h[e]));
+            }
           }
           const int byte = (16 * i + 4 * part) * static_cast<int>(sizeof(S));
           const int g = (byte >> 4) ^ (lane & kSwizzle);
@@ -614,7 +633,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_tile(TileArgs p) {
           const int64_t row = nw + 16 * j + r, m = mw + g * (16 / static_cast<int>(sizeof(S)));
           u32x4 v = *reinterpret_cast<const u32x4*>(mine + r * (kGranules * 16) + (g ^ (r & kSwizzle)) * 16);
           if (row >= p.N) continue;
-          S* to = static_cast<S*>(p.out) + (EPI == kSums ? split * p.out_split : 0) + (row + half * p.N) * p.out_stride + m;
+          S* to = base + (EPI == kSums ? split * p.out_split : 0) + (row + half * p.N) * p.out_stride + m;
           if constexpr (EPI == kSums) {
             if (m >= p.out_stride) continue;          // (rows are whole granules)
             if (p.add) {

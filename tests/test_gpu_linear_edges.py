@@ -185,3 +185,39 @@ def test_outputs_that_share_memory_are_refused():
     g1 = bo.linear_logprobs_grad(both[:, :H], w, tok, r.stats, r.entropy, gl, gh, out=(both[:, H:], torch.empty_like(w)))
     g2 = bo.linear_logprobs_grad(h, w, tok, r.stats, r.entropy, gl, gh)
     assert torch.equal(g1[0], g2.hidden) and torch.equal(g1[1], g2.weight)
+
+
+@pytest.mark.parametrize("T", [45, 600])
+@pytest.mark.parametrize("outlier", [False, True])
+def test_small_rows_beside_large_ones_in_half_precision(T, outlier):
+    """A row's hidden gradient is as exact beside rows whose gradients are 2^28 times
+    its own, or infinite, as by itself."""
+    import torch
+    import paper_2602_10729_amd as bo
+    from test_gpu_linear import Reference
+    _announce("linear f16 rows", T, outlier)
+    V, H = 3000, 64
+    g = _gen(12)
+    w = (0.25 * torch.randn((V, H), generator=g)).half().cuda()
+    h = torch.randn((T, H), generator=g).half().cuda()
+    tok = torch.randint(V, (T,), generator=g).cuda()
+    gl, gh = torch.randn(T, generator=g).cuda(), (0.3 * torch.randn(T, generator=g)).cuda()
+    groups = [(torch.arange(i, T, 3, device="cuda"), s) for i, s in enumerate((2.0 ** 14, 2.0 ** -2, 2.0 ** -14))]
+    for rows, s in groups:
+        gl[rows] *= s
+        gh[rows] *= s
+    r = bo.linear_logprobs(h, w, tok)
+    if outlier:
+        gl[3] = INF
+        groups[0] = (groups[0][0][groups[0][0] != 3], 1.0)
+    got = bo.linear_logprobs_grad(h, w, tok, r.stats, r.entropy, gl, gh)
+    for rows, _ in groups:                           # (a bound over the group's rows alone)
+        few = bo.LinearLogprobsGrad(got.hidden[rows], None)
+        Reference(h[rows], w, tok[rows], 1.0).check_grad(few, gl[rows], gh[rows], "f16", want=(True, False))
+    if not outlier:
+        both = bo.LinearLogprobsGrad(None, got.weight)
+        Reference(h, w, tok, 1.0).check_grad(both, gl, gh, "f16", want=(False, True))
+    for want in ((True, False), (False, True)):
+        one = bo.linear_logprobs_grad(h, w, tok, r.stats, r.entropy, gl, gh, want=want)
+        for a, b, on in zip(one, got, want):
+            assert not on or outlier and a.shape[0] == V or torch.equal(a.nan_to_num(), b.nan_to_num())
