@@ -544,7 +544,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_tile(TileArgs p) {
     // f16 derivatives are held twice: a token's sum over the vocabulary reads them under
     // a scale of its own, a word's sum over the tokens under one that all share (3.84
     // against 3.69 ms with that one alone at 8192 x 32000 x 2048, both gradients, where a
-    // token 2^26 below another's lost what the softmax subtracts).
+    // token 2^28 below another's lost what the softmax subtracts).
     constexpr int kScales = TYPE == BO_TYPE_F16 && EPI == kDerivs ? 2 : 1;
     int common = 0;
     if constexpr (TYPE == BO_TYPE_F16 && EPI != kSums) common = common_exponent(p.largest);

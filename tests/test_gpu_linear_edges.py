@@ -221,3 +221,90 @@ def test_small_rows_beside_large_ones_in_half_precision(T, outlier):
         one = bo.linear_logprobs_grad(h, w, tok, r.stats, r.entropy, gl, gh, want=want)
         for a, b, on in zip(one, got, want):
             assert not on or outlier and a.shape[0] == V or torch.equal(a.nan_to_num(), b.nan_to_num())
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("T", [6, 200])
+def test_rows_with_infinite_logits(T, kind):
+    """A logit of +inf makes its row's results NaN, those of the given token and both
+    gradients among them; other rows' hidden gradients are what they are without it."""
+    import torch
+    import paper_2602_10729_amd as bo
+    _announce("linear +inf", T, kind)
+    V, H, bad = 300, 40, 3
+    g = _gen(11)
+    h = torch.randn((T, H), generator=g).to(_dtype(kind)).cuda()
+    w = (0.3 * torch.randn((V, H), generator=g)).to(_dtype(kind)).cuda()
+    tok = torch.randint(100, V, (T,), generator=g).cuda()
+    gl, gh = torch.randn(T, generator=g).cuda(), (0.3 * torch.randn(T, generator=g)).cuda()
+    h[:, 0], w[:, 0], w[10:50, 0] = 1.0, 0.0, -INF
+    h[bad, 0] = -1.0
+    r = bo.linear_logprobs(h, w, tok)
+    others = torch.arange(T, device="cuda") != bad
+    for out in (r.logprob, r.entropy, r.stats[:, 1]):
+        assert bool(out[bad].isnan()) and not bool(out[others].isnan().any())
+    assert r.stats[bad, 0] == INF
+    got = bo.linear_logprobs_grad(h, w, tok, r.stats, r.entropy, gl, gh)
+    assert bool(got.hidden[bad].isnan().all()) and bool(got.weight.isnan().all())
+    gl[bad] = gh[bad] = 0.0
+    want = bo.linear_logprobs_grad(h, w, tok, r.stats, r.entropy, gl, gh)
+    assert torch.equal(got.hidden[others, 1:], want.hidden[others, 1:])
+    assert not want.hidden[bad].any() and bool(want.hidden[others, 1:].isfinite().all())
+    assert bool(want.weight.isfinite().all()) and not want.weight[10:50].any()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("T", [40, 128])
+def test_few_tokens_with_a_vocabulary_in_pieces(T, kind):
+    """Sums of grad_hidden carried from piece to piece, with d in two parts."""
+    import torch
+    import paper_2602_10729_amd as bo
+    from test_gpu_linear import Reference
+    _announce("linear pieces, few tokens", T, kind)
+    V, H = 2 ** 26 // T + 70_001, 24                 # (a piece is at most 2^28 bytes of d)
+    g = _gen(13)
+    w = (0.4 * torch.randn((V, H), generator=g)).to(_dtype(kind)).cuda()
+    h = torch.randn((T, H), generator=g).to(_dtype(kind)).cuda()
+    tok = torch.randint(V, (T,), generator=g).cuda()
+    tok[0], tok[1], tok[2] = 0, V - 1, -1
+    gl, gh = torch.randn(T, generator=g).cuda(), (0.3 * torch.randn(T, generator=g)).cuda()
+    r = bo.linear_logprobs(h, w, tok)
+    ref = Reference(h, w, tok, 1.0)
+    ref.check(r)
+    ref.check_grad(bo.linear_logprobs_grad(h, w, tok, r.stats, r.entropy, gl, gh), gl, gh, kind)
+
+
+def test_far_gradients():
+    """Both gradients whole, of a matrix past 2^32 bytes."""
+    import torch
+    import paper_2602_10729_amd as bo
+    _announce("linear far gradients")
+    V, H, T = 300_000, 8192, 40
+    g = torch.Generator(device="cuda")
+    g.manual_seed(2)
+    w = torch.empty((V, H), dtype=torch.bfloat16, device="cuda")
+    w.normal_(generator=g).mul_(0.02)
+    h = torch.randn((T, H), generator=g, device="cuda").bfloat16()
+    tok = torch.randint(V, (T,), generator=g, device="cuda")
+    tok[0], tok[1] = V - 1, V - 2
+    gl = torch.randn(T, generator=g, device="cuda")
+    r = bo.linear_logprobs(h, w, tok)
+    got = bo.linear_logprobs_grad(h, w, tok, r.stats, r.entropy, gl)
+    parts = [slice(a, a + 50_000) for a in range(0, V, 50_000)]
+    hd = h.double()
+    x = torch.cat([hd @ w[s].double().T for s in parts], 1)
+    size = float(max((hd.abs() @ w[s].double().abs().T).amax() for s in parts))
+    d = -torch.softmax(x, 1) * gl.double()[:, None]
+    d.scatter_add_(1, tok[:, None], gl.double()[:, None])
+    # d: four logits' errors in its exponent, its own roundings, two parts of 8 bits
+    off = 4 * (2 * H ** 0.5 + 4) * EPS * size + (V / 256 + 64) * EPS + 16 * EPS + 2.0 ** -16
+    hot = torch.zeros_like(d).scatter_(1, tok[:, None], 4 * EPS * gl.double().abs()[:, None])
+    ref, around = torch.zeros_like(hd), torch.zeros_like(hd)
+    for s in parts:
+        ws = w[s].double()
+        ref += d[:, s] @ ws
+        around += (d[:, s].abs() * (off + (2 * V ** 0.5 + 4) * EPS) + hot[:, s]) @ ws.abs()
+        gw = d[:, s].T @ hd
+        tol = (d[:, s].abs() * (off + (2 * T ** 0.5 + 4) * EPS) + hot[:, s]).T @ hd.abs()
+        _close(got.weight[s], gw, tol + 2.0 ** -8 * 1.01 * (gw.abs() + tol) + 1e-36, "grad weight")
+    _close(got.hidden, ref, around + 2.0 ** -8 * 1.01 * (ref.abs() + around) + 1e-36, "grad hidden")

@@ -1,8 +1,10 @@
-"""Expert rows and embeddings where their memory lies: column ranges of one buffer and
-shared memory; on the GPU."""
+"""Expert rows and embeddings where their memory lies: column ranges of one buffer,
+shared memory, and rows past what the caches hold; on the GPU."""
 import pytest
 
 pytestmark = pytest.mark.gpu
+EPS = 2.0 ** -24
+HALF_ULP = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}
 
 
 def _announce(*a):
@@ -122,3 +124,39 @@ def test_outputs_in_the_place_of_vectors_are_refused():
             print("accepted", i, flush=True)
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(keep, held))
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("H", [2112, 2113])
+def test_gradients_past_the_caches(kind, H):
+    """More than 160 MB of rows, which are written past the caches; rows that no pair
+    fills hold NaN and are cleared in the gradient."""
+    import torch
+    import paper_2602_10729_amd as bo
+    _announce("rows, past the caches", kind, H)
+    T, top, E = 20_003, 2, 7
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    draw = lambda *s: torch.randn(s, generator=g, device="cuda")
+    ids = torch.rand((T, E), generator=g, device="cuda").topk(top, 1).indices.int()
+    ids[::9] = -1
+    d = bo.dispatch(ids, E, capacity=5000)
+    kept = int(d.offsets[-1])
+    rows = draw(T * top, H).to(_dtype(kind))
+    rows[kept:] = float("nan")
+    dy, w = draw(T, H).to(_dtype(kind)), draw(T, top)
+    assert rows.numel() * rows.element_size() > 160 << 20
+    got = bo.expert_combine_grad(dy, rows, d.order, d.position, w)
+    pair = d.order[:kept].long()
+    grad = dy[pair // top].double()
+    want = w.view(-1)[pair].double()[:, None] * grad
+    off = (got.rows[:kept].double() - want).abs()
+    assert bool((off <= HALF_ULP[kind] * 1.01 * want.abs() + 2.0 ** -24).all())
+    assert not got.rows[kept:].any()
+    dots = torch.zeros(T * top, dtype=torch.float64, device="cuda")
+    size = torch.zeros_like(dots)
+    dots[pair] = (grad * rows[:kept].double()).sum(1)
+    size[pair] = (grad * rows[:kept].double()).abs().sum(1)
+    assert bool(((got.weights.view(-1).double() - dots).abs() <= (H + 2) * EPS * size).all())
+    again = bo.expert_combine_grad(dy, rows, d.order, d.position, w)
+    assert torch.equal(again.rows, got.rows) and torch.equal(again.weights, got.weights)
