@@ -61,7 +61,8 @@ constexpr int64_t kFewTokens = 128;
 // The shape of the tiles and the splits of k that should take the least time: whole
 // rounds of workgroups, and for split sums their way through memory (4 bytes a
 // picosecond). A k-tile of as many tiles as a compute unit holds at once takes, in
-// microseconds, measured with each shape alone:
+// microseconds, measured with each shape alone (the small one before its sums had two
+// levels); a tile's start and end are not counted:
 constexpr double kTileTime[2][3] = {{1.65, 1.06, 0.96}, {7.2, 3.7, 2.86}};      // 16 bits, fp32; big, middle, small
 struct Choice {
   TileShape tile;
